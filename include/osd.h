@@ -20,6 +20,9 @@
  *                (Section 4.1, mixed sampling).
  *   osd_verify_tree  verification of several candidates per position laid
  *                out as a token tree (the paper's Medusa combination).
+ *   osd_verify_probs  verification against probabilities that the server has
+ *                processed itself (filtered, constrained), with drafts of
+ *                different lengths and drafts without a distribution.
  *
  * Conventions shared by every entry point:
  *   - All array arguments are DEVICE pointers to caller-owned memory on the
@@ -82,7 +85,8 @@ const char *osd_status_string(osd_status status);
  * temperature argument of osd_distill and the OSD_CE loss; 2.1 added
  * osd_distill_accepted; 2.2 added osd_mixed_sample; 2.3 added
  * osd_verify_tree; 2.4 added osd_check_bounded_wait; 2.5 raised
- * osd_mixed_sample's vocabulary limit to OSD_VERIFY_MAX_V. */
+ * osd_mixed_sample's vocabulary limit to OSD_VERIFY_MAX_V; 2.6 added
+ * osd_verify_probs. */
 int osd_abi_version(void);
 
 /*
@@ -300,6 +304,50 @@ osd_status osd_verify_tree(const void *draft_logits, const void *target_logits, 
                            int32_t *accepted, int32_t *path, int32_t *out_tokens,
                            int32_t *last_node, float *diag_margin, float *diag_cdf_gap,
                            void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Speculative-sampling verification against given probabilities (Section 3,
+ * Appendix A.1): osd_verify's tests and draw for servers whose p and q are not
+ * a plain softmax, because they filter (top-k, top-p, min-p), penalise or
+ * constrain them first, whose drafts come without a distribution (looked up in
+ * the prompt, or the draft model's argmax), or whose sequences carry drafts of
+ * different lengths.
+ *
+ * For each sequence b, with n = draft_lens[b] (k without draft_lens), p_i the
+ * target row i and q_i the draft row i (without draft_probs 1 at draft_tokens[b,i]
+ * and 0 elsewhere):
+ *   - tests i = 0..n-1 in order and accepts draft_tokens[b,i] iff
+ *     uniforms[b,i] q_i(y_i) < p_i(y_i), the product taken exactly (q(y) = 0 <
+ *     p(y) accepts, p(y) = 0 does not), stopping at the first rejection; a =
+ *     number accepted;
+ *   - draws one more token by inverse CDF with uniforms[b,k] from the weights
+ *     w = max(0, p_a - q_a) if a < n, w = p_n if a = n, as osd_verify does:
+ *     min{ j : C_j > u W } in ascending order, the largest j with w_j > 0 if
+ *     there is none, the first maximum of p_a if W = 0.  Rows need not sum to 1.
+ * The sums are exact: every probability counts as a multiple of 2^-62, to which
+ * it is rounded once, so the token depends on no order of summation.
+ *
+ * draft_probs    row (b, i) starts at base + b*d_stride_b + i*d_stride_i
+ *                elements, V contiguous entries; i < k.  Nullable.
+ * target_probs   the same with t_stride_b, t_stride_i; i <= k
+ * draft_tokens   [B, k] int32; entries i >= n are not read
+ * draft_lens     [B] int32 in 0..k, nullable (NULL = k everywhere)
+ * uniforms       [B, k+1] fp32 in [0, 1); u[b, k] drives the draw
+ * accepted       [B]          out: a in 0..n; -1 (tokens -1, mask 0) if a draft
+ *                             token lies outside [0, V), draft_lens[b] outside
+ *                             [0, k], or a bounded wait gave up (as osd_verify)
+ * out_tokens     [B, k+1]     out: y_0..y_{a-1}, the drawn token at a, then -1
+ * mismatch_mask  [B, k]       out: 1 at i == a when a < n, else 0
+ * Probabilities are >= 0 and < 2 and a row's sum is below 4; with others the
+ * token drawn is unspecified, but in [0, V).
+ * Limits: 0 <= k <= OSD_VERIFY_MAX_K (k = 0 draws one token a row),
+ * 1 <= V <= OSD_VERIFY_MAX_V, B >= 0, strides >= 0.  No workspace.
+ */
+osd_status osd_verify_probs(const void *draft_probs, const void *target_probs, osd_dtype dtype,
+                            int B, int k, int V, int64_t d_stride_b, int64_t d_stride_i,
+                            int64_t t_stride_b, int64_t t_stride_i, const int32_t *draft_tokens,
+                            const int32_t *draft_lens, const float *uniforms, int32_t *accepted,
+                            int32_t *out_tokens, uint8_t *mismatch_mask, void *stream);
 
 /*
  * Mixed-token sampling (Section 4.1): one token per position from the mixture

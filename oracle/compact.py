@@ -1,0 +1,65 @@
+"""Oracle of the operations on compact targets (test infrastructure, as the package is):
+plain numpy in 64 bits, one row or sequence at a time, straight from the definitions.
+It shares no code with the CUDA path."""
+from __future__ import annotations
+
+import numpy as np
+
+
+def _f64(x):
+    """Any float array or tensor as float64 (exact for fp32 and bf16)."""
+    if x is None:
+        return None
+    if hasattr(x, "detach"):
+        x = x.detach().cpu().double().numpy()
+    return np.asarray(x, np.float64)
+
+
+def units(p):
+    """Probabilities as whole multiples of 2^-62, rounded to nearest, ties to even."""
+    return np.rint(np.ldexp(_f64(p), 62)).astype(np.uint64)
+
+
+def draw(weights, u):
+    """min{ j : C_j > u W } of whole weights, in exact integers; the largest j with weight if
+    there is none; None if nothing has weight."""
+    W = int(weights.sum(dtype=np.uint64))
+    if W == 0:
+        return None
+    num, den = float(u).as_integer_ratio()
+    C = np.cumsum(weights, dtype=np.uint64)
+    if num < den:
+        tau = max(num, 0) * W // den  # C_j > u W if and only if C_j > floor(u W)
+        return int(np.searchsorted(C, np.uint64(tau), side="right"))
+    return int(np.nonzero(weights)[0][-1])
+
+
+def verify_probs(q, p, tokens, uniforms, lens=None):
+    """osd_verify_probs (include/osd.h): (accepted, out_tokens, mismatch_mask)."""
+    q, p, u = _f64(q), _f64(p), _f64(uniforms)
+    B, k1, V = p.shape
+    k = k1 - 1
+    y = np.asarray(tokens, np.int64).reshape(B, k)
+    acc = np.full(B, -1, np.int32)
+    out, mask = np.full((B, k1), -1, np.int32), np.zeros((B, k), np.uint8)
+    for b in range(B):
+        n = k if lens is None else int(lens[b])
+        if not 0 <= n <= k or np.any(y[b, :n] < 0) or np.any(y[b, :n] >= V):
+            continue
+        a = 0
+        while a < n:
+            qy = 1.0 if q is None else q[b, a, y[b, a]]
+            if not u[b, a] * qy < p[b, a, y[b, a]]:  # the product of two fp32 numbers is exact
+                break
+            a += 1
+        P = units(p[b, a])
+        w = P
+        if a < n:
+            Q = units(q[b, a]) if q is not None else units(np.arange(V) == y[b, a])
+            w = np.where(P > Q, P - np.minimum(P, Q), np.uint64(0))
+            mask[b, a] = 1
+        j = draw(w, u[b, k])
+        acc[b] = a
+        out[b, :a] = y[b, :a]
+        out[b, a] = int(np.argmax(p[b, a])) if j is None else j
+    return acc, out, mask

@@ -36,7 +36,7 @@ VERIFY_MAX_V = 1 << 21
 # every symbol include/osd.h declares
 EXPORTS = ("osd_status_string", "osd_abi_version", "osd_verify_workspace_size",
            "osd_verify", "osd_verify_noalloc", "osd_distill", "osd_distill_accepted",
-           "osd_mixed_sample", "osd_verify_tree_workspace_size", "osd_verify_tree", "osd_check_bounded_wait")
+           "osd_verify_probs", "osd_mixed_sample", "osd_verify_tree_workspace_size", "osd_verify_tree", "osd_check_bounded_wait")
 
 
 class OsdError(RuntimeError):
@@ -80,6 +80,8 @@ def load_library():
     lib.osd_verify_tree.restype = i32
     lib.osd_verify_tree.argtypes = [vp, vp, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_int32), vp, vp, f32,
                                     vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.osd_verify_probs.restype = i32
+    lib.osd_verify_probs.argtypes = [vp, vp, i32, i32, i32, i32, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp]
     lib.osd_check_bounded_wait.restype = i32
     lib.osd_check_bounded_wait.argtypes = [ctypes.c_uint32, vp, vp, vp]
     lib.osd_mixed_sample.restype = i32
@@ -98,7 +100,7 @@ class _NoBinding:
     def _none(*args):
         return None
 
-    verify = distill = distill_accepted = mixed_sample = verify_tree = _none
+    verify = verify_probs = distill = distill_accepted = mixed_sample = verify_tree = _none
 
 
 def _load_binding():
@@ -256,6 +258,58 @@ def osd_verify_noalloc(draft_logits: torch.Tensor, target_logits: torch.Tensor, 
                                     _ptr(out.diag_cdf_gap), _stream(dev, stream))
     if st != OSD_OK:
         raise OsdError(st, "osd_verify_noalloc")
+    return out
+
+
+def osd_verify_probs(draft_probs: Optional[torch.Tensor], target_probs: torch.Tensor, draft_tokens: torch.Tensor,
+                     uniforms: torch.Tensor, *, draft_lens: Optional[torch.Tensor] = None,
+                     out: Optional[VerifyResult] = None, stream: Optional[torch.cuda.Stream] = None) -> VerifyResult:
+    """Speculative-sampling verification against given probabilities (Appendix A.1); see
+    include/osd.h.
+
+    ``target_probs`` [B,k+1,V] and ``draft_probs`` [B,k,V] are views with contiguous rows
+    and of one dtype; ``draft_probs`` None means that every draft was proposed with
+    certainty.  ``draft_lens`` [B] int32 gives each sequence's number of drafts, k where it
+    is None.  The result's diagnostics are None; ``out`` may be preallocated.
+    """
+    r = (_binding or _load_binding()).verify_probs(draft_probs, target_probs, draft_tokens, uniforms, draft_lens, out,
+                                                   stream)
+    if r is not None:
+        return _native("osd_verify_probs", r)
+    lib = load_library()
+    dev = _need_cuda(draft_probs, target_probs, draft_tokens, uniforms, draft_lens, *(out or ()))
+    if target_probs.dim() != 3 or target_probs.shape[1] < 1:
+        raise ValueError("target_probs must be [B, k+1, V]")
+    B, k1, V = target_probs.shape
+    k = k1 - 1
+    if draft_probs is not None and (tuple(draft_probs.shape) != (B, k, V) or draft_probs.dtype != target_probs.dtype):
+        raise ValueError("draft_probs must be [B, k, V] with the target's dtype")
+    for t in (draft_probs, target_probs):
+        if t is not None and V > 1 and t.stride(-1) != 1:
+            raise ValueError("the vocabulary dimension must be contiguous")
+    if draft_tokens.dtype != torch.int32 or tuple(draft_tokens.shape) != (B, k) or not draft_tokens.is_contiguous():
+        raise ValueError("draft_tokens must be contiguous int32 [B, k]")
+    if uniforms.dtype != torch.float32 or tuple(uniforms.shape) != (B, k1) or not uniforms.is_contiguous():
+        raise ValueError("uniforms must be contiguous float32 [B, k+1]")
+    if draft_lens is not None and (draft_lens.dtype != torch.int32 or tuple(draft_lens.shape) != (B,)
+                                   or not draft_lens.is_contiguous()):
+        raise ValueError("draft_lens must be contiguous int32 [B]")
+    if out is None:
+        out = VerifyResult(torch.empty(B, dtype=torch.int32, device=dev),
+                           torch.empty(B, k1, dtype=torch.int32, device=dev),
+                           torch.empty(B, k, dtype=torch.uint8, device=dev), None, None)
+    for t, dtype, shape in ((out.accepted, torch.int32, (B,)), (out.out_tokens, torch.int32, (B, k1)),
+                            (out.mismatch_mask, torch.uint8, (B, k))):
+        if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError("out must hold contiguous int32 [B], int32 [B, k+1] and uint8 [B, k]")
+    ds = (0, 0) if draft_probs is None else (draft_probs.stride(0), draft_probs.stride(1))
+    with _on(dev):
+        st = lib.osd_verify_probs(_ptr(draft_probs), _ptr(target_probs), _dtype_code(target_probs), B, k, V, *ds,
+                                  target_probs.stride(0), target_probs.stride(1), _ptr(draft_tokens), _ptr(draft_lens),
+                                  _ptr(uniforms), _ptr(out.accepted), _ptr(out.out_tokens), _ptr(out.mismatch_mask),
+                                  _stream(dev, stream))
+    if st != OSD_OK:
+        raise OsdError(st, "osd_verify_probs")
     return out
 
 

@@ -216,6 +216,58 @@ PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// draft, target, tokens, uniforms, lens, out, stream
+PyObject* verify_probs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 7) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject* {
+        Call c;
+        const at::Tensor* target = c.tensor(a[1]);
+        if (!c.ok || target->dim() != 3 || target->size(1) < 1) Py_RETURN_NONE;
+        const int64_t B = target->size(0), k = target->size(1) - 1, V = target->size(2);
+        const at::Tensor *draft = c.optional(a[0]), *tokens = c.tensor(a[2]), *uniforms = c.tensor(a[3]),
+                         *lens = c.optional(a[4]);
+        const int dt = dtype_code(*target);
+        if (!c.need(dt >= 0 && (V <= 1 || target->stride(2) == 1))) Py_RETURN_NONE;
+        if (draft)
+            c.need(draft->scalar_type() == target->scalar_type() && draft->sizes() == at::IntArrayRef({B, k, V}) &&
+                   (V <= 1 || draft->stride(2) == 1));
+        c.need(tokens->scalar_type() == at::kInt && shaped(*tokens, {B, k}));
+        c.need(uniforms->scalar_type() == at::kFloat && shaped(*uniforms, {B, k + 1}));
+        if (lens) c.need(lens->scalar_type() == at::kInt && shaped(*lens, {B}));
+        void* stream = c.stream(a[6]);
+        if (!c.ok) Py_RETURN_NONE;
+        const at::Tensor* o[3] = {};
+        at::Tensor made[5];
+        const bool own = a[5] == Py_None;
+        if (!own) {
+            if (!c.need(Py_TYPE(a[5]) == reinterpret_cast<PyTypeObject*>(g_verify_result))) Py_RETURN_NONE;
+            for (int i = 0; i < 3; ++i) o[i] = c.member(a[5], i);
+            if (!c.need(o[0] && o[1] && o[2])) Py_RETURN_NONE;
+            c.need(o[0]->scalar_type() == at::kInt && shaped(*o[0], {B}));
+            c.need(o[1]->scalar_type() == at::kInt && shaped(*o[1], {B, k + 1}));
+            if (!c.need(o[2]->scalar_type() == at::kByte && shaped(*o[2], {B, k}))) Py_RETURN_NONE;
+        } else {
+            made[0] = fresh({B}, at::kInt, c.dev);
+            made[1] = fresh({B, k + 1}, at::kInt, c.dev);
+            made[2] = fresh({B, k}, at::kByte, c.dev);
+            for (int i = 0; i < 3; ++i) o[i] = &made[i];
+        }
+        const void *qp = ptr(draft), *pp = ptr(target);
+        const int64_t qb = draft ? draft->stride(0) : 0, qi = draft ? draft->stride(1) : 0, pb = target->stride(0),
+                      pi = target->stride(1);
+        const auto *yp = static_cast<const int32_t*>(ptr(tokens)), *np = static_cast<const int32_t*>(ptr(lens));
+        const auto* up = static_cast<const float*>(ptr(uniforms));
+        auto *ap = static_cast<int32_t*>(ptr(o[0])), *tp = static_cast<int32_t*>(ptr(o[1]));
+        auto* mp = static_cast<uint8_t*>(ptr(o[2]));
+        const osd_status st = released([&]() {
+            return osd_verify_probs(qp, pp, osd_dtype(dt), int(B), int(k), int(V), qb, qi, pb, pi, yp, np, up, ap, tp, mp,
+                                    stream);
+        });
+        if (st != OSD_OK) return PyLong_FromLong(st);
+        return own ? result(g_verify_result, made, 5) : Py_NewRef(a[5]);
+    });
+}
+
 // A [N, V] or [G, P, V] view with contiguous rows.
 struct Rows {
     int64_t G, P, V, sg, sp;
@@ -443,6 +495,7 @@ PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr
 PyMethodDef methods[] = {{"setup", FAST(setup)},
                          {"verify", FAST(verify)},
+                         {"verify_probs", FAST(verify_probs)},
                          {"distill", FAST(distill)},
                          {"distill_accepted", FAST(distill_accepted)},
                          {"mixed_sample", FAST(mixed_sample)},

@@ -1,0 +1,48 @@
+"""Refusals of the operations on compact targets: answered on the host, before any pointer is
+touched, by the C ABI and by the Python functions."""
+import ctypes
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def osd():
+    import paper_2310_07177_gb300 as pkg
+    pkg.build_library()
+    pkg.load_library()
+    return pkg
+
+
+FAKE = ctypes.c_void_p(0x1000)  # never dereferenced: every call below fails validation first
+ODD = ctypes.c_void_p(0x1001)
+
+
+def _verify_probs(osd, **kw):
+    a = dict(q=FAKE, p=FAKE, dtype=0, B=2, k=2, V=16, dsb=32, dsi=16, tsb=48, tsi=16, y=FAKE, n=None, u=FAKE, acc=FAKE,
+             out=FAKE, mask=FAKE, stream=None)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return osd.load_library().osd_verify_probs(*a.values())
+
+
+def test_verify_probs_refusals(osd):
+    bad, beyond = osd.OSD_ERR_INVALID_ARG, osd.OSD_ERR_UNSUPPORTED
+    for kw in ({"dtype": 2}, {"dtype": -1}, {"B": -1}, {"k": -1}, {"V": 0}, {"dsb": -1}, {"dsi": -1}, {"tsb": -1},
+               {"tsi": -1}, {"p": None}, {"u": None}, {"acc": None}, {"out": None}, {"y": None}, {"mask": None},
+               {"p": ODD}, {"q": ODD}, {"p": ODD, "dtype": 1}, {"y": ODD}, {"n": ODD}, {"u": ODD}, {"acc": ODD}, {"out": ODD}):
+        assert _verify_probs(osd, **kw) == bad, kw
+    assert _verify_probs(osd, k=65) == beyond
+    assert _verify_probs(osd, V=(1 << 21) + 1) == beyond
+    # an empty batch does nothing
+    assert _verify_probs(osd, B=0, p=None, q=None, y=None, u=None, acc=None, out=None, mask=None) == osd.OSD_OK
+
+
+def test_python_takes_cuda_tensors_only(osd):
+    p, y, u = torch.zeros(2, 3, 8), torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, 3)
+    with pytest.raises(ValueError, match="CUDA tensors only"):
+        osd.osd_verify_probs(None, p, y, u)
+
+
+def test_version(osd):
+    assert osd.osd_abi_version() >= (2 << 16) | 6

@@ -1,0 +1,219 @@
+"""osd_verify_probs against the oracle.  All its arithmetic is exact (products of two fp32
+numbers, sums of whole multiples of 2^-62), so every result has to be equal."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import compact
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def osd():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA GPU")
+    import paper_2310_07177_gb300 as pkg
+    pkg.build_library()
+    pkg.load_library()
+    return pkg
+
+
+def _inputs(B, k, V, dtype, seed, accept=0.6, minp=0.0, std=2.5):
+    """p = accept q + (1 - accept) r, drafts from q; with minp p's small entries are cut to zero."""
+    g = torch.Generator().manual_seed(seed)
+    q = torch.softmax(torch.randn(B, k + 1, V, generator=g) * std, -1)
+    p = accept * q + (1 - accept) * torch.softmax(torch.randn(B, k + 1, V, generator=g) * std, -1)
+    if minp:
+        p = torch.where(p >= minp * p.amax(-1, keepdim=True), p, 0.0)
+        p /= p.sum(-1, keepdim=True)
+    y = torch.multinomial(q[:, :k].reshape(B * k, V), 1, generator=g).view(B, k).int() if k else torch.zeros(B, 0).int()
+    return q[:, :k].to(dtype), p.to(dtype), y, torch.rand(B, k + 1, generator=g)
+
+
+def _check(osd, q, p, y, u, lens=None, **kw):
+    dev = lambda t: None if t is None else t.cuda()
+    got = osd.osd_verify_probs(dev(q), dev(p), dev(y), dev(u), draft_lens=dev(lens), **kw)
+    torch.cuda.synchronize()
+    ref = compact.verify_probs(q, p, y.numpy(), u, None if lens is None else lens.numpy())
+    for name, a, b in zip(("accepted", "out_tokens", "mismatch_mask"), got, ref):
+        np.testing.assert_array_equal(a.cpu().numpy(), b, err_msg=name)
+    return ref
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [1, 2, 7, 33, 256, 1003, 4096, 8197])
+def test_small(osd, V, dtype):
+    for seed, (B, k) in enumerate([(1, 1), (5, 3), (3, 8), (2, 0)]):
+        q, p, y, u = _inputs(B, k, V, dtype, 100 * V + seed)
+        _check(osd, q, p, y, u)
+        _check(osd, None, p, y, u)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,k,V", [(4, 4, 32000), (40, 3, 32001), (2, 2, 128256), (1, 1, 160001), (3, 64, 515), (150, 2, 5000),
+                                   (350, 1, 2050)])
+def test_sizes(osd, B, k, V, dtype):
+    for accept, minp in ((0.3, 0.0), (0.95, 0.02)):
+        q, p, y, u = _inputs(B, k, V, dtype, B + k + V, accept, minp)
+        ref = _check(osd, q, p, y, u)
+        _check(osd, None, p, y, u)
+    assert B < 10 or len(set(ref[0].tolist())) > 1
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_ragged(osd, dtype):
+    q, p, y, u = _inputs(60, 5, 3001, dtype, 3, 0.8)
+    lens = torch.randint(0, 6, (60,), generator=torch.Generator().manual_seed(1)).int()
+    y = torch.where(torch.arange(5) < lens[:, None], y, -7)  # padding is not read
+    _check(osd, q, p, y, u, lens)
+    _check(osd, None, p, y, u, lens)
+    _check(osd, q, p, y, u, torch.zeros(60).int())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_strided_views(osd, dtype):
+    """Positions and sequences of larger tensors, in another order, off the 16-byte grid."""
+    q, p, y, u = _inputs(6, 3, 1001, dtype, 4)
+    wide = torch.zeros(4, 6, 1010, dtype=dtype, device="cuda")  # [k+1, B, V + 9]
+    wide[:, :, 5:1006] = p.transpose(0, 1).cuda()
+    narrow = torch.zeros(6, 3, 1003, dtype=dtype, device="cuda")
+    narrow[:, :, 1:1002] = q.cuda()
+    got = osd.osd_verify_probs(narrow[:, :, 1:1002], wide[:, :, 5:1006].transpose(0, 1), y.cuda(), u.cuda())
+    ref = compact.verify_probs(q, p, y.numpy(), u)
+    for a, b in zip(got, ref):
+        np.testing.assert_array_equal(a.cpu().numpy(), b)
+    # one row for all sequences and positions
+    one = p[:1, :1].cuda().expand(6, 4, 1001)
+    got = osd.osd_verify_probs(q.cuda(), one, y.cuda(), u.cuda())
+    ref = compact.verify_probs(q, p[:1, :1].expand(6, 4, 1001), y.numpy(), u)
+    for a, b in zip(got, ref):
+        np.testing.assert_array_equal(a.cpu().numpy(), b)
+
+
+def test_edges_of_the_draw(osd):
+    """Uniforms on the edges of dyadic prefix sums, 0, the largest below 1, and 1; a bonus draw."""
+    V = 4096
+    us = torch.tensor([0.0, 2.0 ** -30, 0.25, 0.25 - 2.0 ** -26, 0.5, 0.75, 1 - 2.0 ** -24, 1.0, 1.5])
+    for dtype in (torch.float32, torch.bfloat16):
+        p = torch.full((len(us), 1, V), 1.0 / V).to(dtype)
+        _check(osd, None, p, torch.zeros(len(us), 0).int(), us[:, None])
+        p[:, :, 100:4000] = 0  # zero weights are never drawn
+        _check(osd, None, p, torch.zeros(len(us), 0).int(), us[:, None])
+
+
+def test_equal_tiny_and_missing_mass(osd):
+    """Rows of equal probabilities (no residual), weights far below the largest, rows that do not
+    sum to 1, and all-zero rows."""
+    V = 3000
+    g = torch.Generator().manual_seed(9)
+    base = torch.softmax(torch.randn(V, generator=g) * 3, -1)
+    rows = [(base, base), (base * 0.5, base), (base * 0.5, base * 0.5), (torch.zeros(V), base), (base, torch.zeros(V)),
+            (base * 1e-9, torch.zeros(V)), (base * 1e-9, base * 1e-9 * (torch.rand(V, generator=g) + 0.5)),
+            (torch.where(torch.arange(V) == 2999, 1.0, base * 2.0 ** -40), torch.zeros(V)),
+            (base + 2.0 ** -24, base), (base * 1.9, base * 1.1)]
+    p = torch.stack([r[0] for r in rows])[:, None].repeat(1, 2, 1)
+    q = torch.stack([r[1] for r in rows])[:, None]
+    y = torch.full((len(rows), 1), int(base.argmax())).int()
+    for u0, u1 in ((0.3, 0.4), (0.9, 0.7), (0.999999, 0.0), (0.5, 0.999999)):
+        u = torch.tensor([[u0, u1]]).expand(len(rows), 2).contiguous()
+        for dtype in (torch.float32, torch.bfloat16):
+            _check(osd, q.to(dtype), p.to(dtype), y, u)
+            _check(osd, None, p.to(dtype), y, u)
+
+
+def test_bad_sequences(osd):
+    q, p, y, u = _inputs(6, 3, 500, torch.float32, 5)
+    y[0, 0], y[1, 2], y[2, 1] = -1, 500, 1 << 30
+    lens = torch.tensor([3, 3, 3, 4, -1, 2]).int()
+    ref = _check(osd, q, p, y, u, lens)
+    assert (ref[0][:5] == -1).all() and ref[0][5] >= 0
+
+
+def test_outside_the_domain_stays_in_range(osd):
+    """NaN, infinite, negative and large entries: an unspecified token, but a token."""
+    for dtype in (torch.float32, torch.bfloat16):
+        q, p, y, u = (t.cuda() for t in _inputs(8, 2, 2001, dtype, 6))
+        for i, x in enumerate((float("nan"), float("inf"), -1.0, 5.0, 1e30, -float("inf"))):
+            p[i, :, ::7] = x
+            q[7 - i, :, ::5] = x
+        p[6] = float("nan")
+        p[7] = float("inf")
+        for qq in (q, None):
+            acc, out, _ = (t.cpu() for t in osd.osd_verify_probs(qq, p, y, u)[:3])
+            assert ((acc >= 0) & (acc <= 2)).all()
+            at = out.gather(1, acc[:, None].long())
+            assert ((at >= 0) & (at < 2001)).all()
+
+
+def test_offsets_past_32_bits(osd):
+    """Rows more than 2^31 entries apart."""
+    V, far = 1500, (1 << 31) + 8 * 11
+    q, p, y, u = _inputs(2, 1, V, torch.bfloat16, 7)
+    whole = torch.zeros(far + 4 * V, dtype=torch.bfloat16, device="cuda")
+    view = whole.as_strided((2, 2, V), (far, V, 1))
+    view.copy_(p.cuda())
+    got = osd.osd_verify_probs(q.cuda(), view, y.cuda(), u.cuda())
+    for a, b in zip(got, compact.verify_probs(q, p, y.numpy(), u)):
+        np.testing.assert_array_equal(a.cpu().numpy(), b)
+
+
+def test_graph_streams_and_given_outputs(osd):
+    """Captured, replayed on new inputs, and on a side stream into the caller's buffers."""
+    first, second = _inputs(20, 4, 9000, torch.float32, 8), _inputs(20, 4, 9000, torch.float32, 9)
+    static = [t.cuda() for t in first]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        osd.osd_verify_probs(*static)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        res = osd.osd_verify_probs(*static)
+        again = osd.osd_verify_probs(None, *static[1:])
+    for inputs in (second, first):
+        for s, t in zip(static, inputs):
+            s.copy_(t)
+        graph.replay()
+        torch.cuda.synchronize()
+        q, p, y, u = inputs
+        for r, qq in ((res, q), (again, None)):
+            for a, b in zip(r, compact.verify_probs(qq, p, y.numpy(), u)):
+                np.testing.assert_array_equal(a.cpu().numpy(), b)
+    out = osd.VerifyResult(torch.full((20,), 9, dtype=torch.int32, device="cuda"),
+                           torch.full((20, 5), 9, dtype=torch.int32, device="cuda"),
+                           torch.full((20, 4), 9, dtype=torch.uint8, device="cuda"), None, None)
+    side.wait_stream(torch.cuda.current_stream())
+    got = osd.osd_verify_probs(*static, out=out, stream=side)
+    side.synchronize()
+    assert got is out and torch.equal(out.out_tokens, res.out_tokens) and torch.equal(out.accepted, res.accepted)
+
+
+def test_native_equals_ctypes_and_refusals(osd, monkeypatch):
+    q, p, y, u = (t.cuda() for t in _inputs(7, 3, 700, torch.bfloat16, 10))
+    a = osd.osd_verify_probs(q, p, y, u)
+    real = osd._binding
+    assert real.verify_probs(q, p, y, u, None, None, None) is not None
+
+    class Nothing:
+        def __getattr__(self, name):
+            return lambda *args: None
+    monkeypatch.setattr(osd, "_binding", Nothing())
+    b = osd.osd_verify_probs(q, p, y, u)
+    for s, t in zip(a[:3], b[:3]):
+        assert s.dtype == t.dtype and torch.equal(s, t)
+    monkeypatch.setattr(osd, "_binding", real)
+    with pytest.raises(ValueError, match="int32"):
+        osd.osd_verify_probs(q, p, y.long(), u)
+    with pytest.raises(ValueError, match="draft_probs"):
+        osd.osd_verify_probs(q.float(), p, y, u)
+    with pytest.raises(ValueError, match="contiguous"):
+        osd.osd_verify_probs(q, p.transpose(1, 2).contiguous().transpose(1, 2), y, u)
+    with pytest.raises(ValueError, match="uniforms"):
+        osd.osd_verify_probs(q, p, y, u[:, :3].contiguous())
+    with pytest.raises(ValueError, match="draft_lens"):
+        osd.osd_verify_probs(q, p, y, u, draft_lens=torch.zeros(3, dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError, match="out must"):
+        osd.osd_verify_probs(q, p, y, u, out=osd.VerifyResult(a.accepted[:3], a.out_tokens, a.mismatch_mask, None, None))
+    with pytest.raises(TypeError, match="float32 or bfloat16"):
+        osd.osd_verify_probs(q.half(), p.half(), y, u)
