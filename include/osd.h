@@ -23,6 +23,8 @@
  *   osd_verify_probs  verification against probabilities that the server has
  *                processed itself (filtered, constrained), with drafts of
  *                different lengths and drafts without a distribution.
+ *   osd_topk     the top logits of target rows and the log of the mass of the
+ *                rest: the compact form in which buffer R keeps a row.
  *
  * Conventions shared by every entry point:
  *   - All array arguments are DEVICE pointers to caller-owned memory on the
@@ -86,7 +88,7 @@ const char *osd_status_string(osd_status status);
  * osd_distill_accepted; 2.2 added osd_mixed_sample; 2.3 added
  * osd_verify_tree; 2.4 added osd_check_bounded_wait; 2.5 raised
  * osd_mixed_sample's vocabulary limit to OSD_VERIFY_MAX_V; 2.6 added
- * osd_verify_probs. */
+ * osd_verify_probs and osd_topk. */
 int osd_abi_version(void);
 
 /*
@@ -348,6 +350,37 @@ osd_status osd_verify_probs(const void *draft_probs, const void *target_probs, o
                             int64_t t_stride_b, int64_t t_stride_i, const int32_t *draft_tokens,
                             const int32_t *draft_lens, const float *uniforms, int32_t *accepted,
                             int32_t *out_tokens, uint8_t *mismatch_mask, void *stream);
+
+/* Largest number of entries osd_topk takes of a row. */
+#define OSD_TOPK_MAX_K 1024
+
+/*
+ * The K largest logits of each row, with their ids and the mass of all other
+ * entries: the compact form of a target row.  Algorithm 1 keeps the target's
+ * distribution at every rejected position in the buffer R until the draft is
+ * updated; a row of 32000 bf16 logits takes 64000 bytes, its top 64 take 516.
+ *
+ * logits         rows laid out as in osd_distill: row (g, p) starts at base +
+ *                g*stride_g + p*stride_p elements
+ * mask           [G, P] uint8, nullable (NULL = every row active); outputs of
+ *                inactive rows are not written
+ * K              1 <= K <= min(V, OSD_TOPK_MAX_K)
+ * temperature    tau > 0 and finite: of `rest` only
+ * values         [G, P, K] fp32 out: the K largest logits (exact), descending;
+ *                of equal ones the lower ids, first (-0 equals 0)
+ * ids            [G, P, K] int32 out: their vocabulary indices
+ * rest           [G, P] fp32 out, nullable: the natural logarithm of the sum of
+ *                exp(x / tau) over the entries not taken; -inf where they are
+ *                all -inf or there are none
+ * status         nullable device int32, as in osd_distill (rows whose copy did
+ *                not arrive in time get ids of -1)
+ * -inf logits are ordinary entries that sort last.  Rows that hold NaN or +inf
+ * are outside the domain: their results are unspecified (ids of -1 may occur).
+ * Limits: 1 <= V <= OSD_VERIFY_MAX_V, strides >= 0.  No workspace.
+ */
+osd_status osd_topk(const void *logits, osd_dtype dtype, int G, int P, int V, int64_t stride_g,
+                    int64_t stride_p, const uint8_t *mask, int K, float temperature, float *values,
+                    int32_t *ids, float *rest, int32_t *status, void *stream);
 
 /*
  * Mixed-token sampling (Section 4.1): one token per position from the mixture

@@ -63,3 +63,17 @@ def verify_probs(q, p, tokens, uniforms, lens=None):
         out[b, :a] = y[b, :a]
         out[b, a] = int(np.argmax(p[b, a])) if j is None else j
     return acc, out, mask
+
+
+def topk(logits, K, temperature=1.0):
+    """osd_topk of rows [N, V]: (values, ids, rest), sorted by value descending, then by id."""
+    x = _f64(logits)
+    ids = np.argsort(-x, axis=1, kind="stable")
+    top = ids[:, :K]
+    values = np.take_along_axis(x, top, 1)
+    rest = np.full(len(x), -np.inf)
+    for n, row in enumerate(x):
+        o = row[ids[n, K:]] / temperature
+        if o.size and o[0] > -np.inf:  # o[0] is the largest of them
+            rest[n] = o[0] + np.log(np.exp(o - o[0]).sum())
+    return values, top.astype(np.int32), rest

@@ -32,11 +32,12 @@ OSD_F32, OSD_BF16 = 0, 1
 LOSS_KINDS = {"fkl": 0, "rkl": 1, "jsd": 2, "tvd": 3, "ce": 4}
 VERIFY_MAX_K = 64
 VERIFY_MAX_V = 1 << 21
+TOPK_MAX_K = 1024
 
 # every symbol include/osd.h declares
 EXPORTS = ("osd_status_string", "osd_abi_version", "osd_verify_workspace_size",
            "osd_verify", "osd_verify_noalloc", "osd_distill", "osd_distill_accepted",
-           "osd_verify_probs", "osd_mixed_sample", "osd_verify_tree_workspace_size", "osd_verify_tree", "osd_check_bounded_wait")
+           "osd_verify_probs", "osd_topk", "osd_mixed_sample", "osd_verify_tree_workspace_size", "osd_verify_tree", "osd_check_bounded_wait")
 
 
 class OsdError(RuntimeError):
@@ -82,6 +83,8 @@ def load_library():
                                     vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.osd_verify_probs.restype = i32
     lib.osd_verify_probs.argtypes = [vp, vp, i32, i32, i32, i32, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+    lib.osd_topk.restype = i32
+    lib.osd_topk.argtypes = [vp, i32, i32, i32, i32, i64, i64, vp, i32, f32, vp, vp, vp, vp, vp]
     lib.osd_check_bounded_wait.restype = i32
     lib.osd_check_bounded_wait.argtypes = [ctypes.c_uint32, vp, vp, vp]
     lib.osd_mixed_sample.restype = i32
@@ -100,7 +103,7 @@ class _NoBinding:
     def _none(*args):
         return None
 
-    verify = verify_probs = distill = distill_accepted = mixed_sample = verify_tree = _none
+    verify = verify_probs = distill = distill_accepted = mixed_sample = verify_tree = topk = _none
 
 
 def _load_binding():
@@ -116,7 +119,7 @@ def _load_binding():
     loader = importlib.machinery.ExtensionFileLoader("_binding", BINDING_PATH)
     mod = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_binding", BINDING_PATH, loader=loader))
     loader.exec_module(mod)
-    mod.setup(VerifyResult, DistillAcceptedResult, TreeResult)
+    mod.setup(VerifyResult, DistillAcceptedResult, TreeResult, TopkResult)
     _binding = mod
     return mod
 
@@ -416,6 +419,52 @@ def osd_distill_accepted(draft_logits: torch.Tensor, target_logits: torch.Tensor
                                       _stream(dev, stream))
     if st != OSD_OK:
         raise OsdError(st, "osd_distill_accepted")
+    return out
+
+
+class TopkResult(NamedTuple):
+    """The compact form of target rows: osd_topk's outputs, osd_distill_topk's teacher."""
+    values: torch.Tensor          # [.., K] fp32, descending
+    ids: torch.Tensor             # [.., K] int32
+    rest: Optional[torch.Tensor]  # [..] fp32: log of the other entries' sum of exp(x / temperature)
+
+
+def osd_topk(logits: torch.Tensor, K: int, mask: Optional[torch.Tensor] = None, *, temperature: float = 1.0,
+             rest: bool = True, out: Optional[TopkResult] = None, status: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None) -> TopkResult:
+    """The K largest logits of each row, their ids and the log-mass of the others (see
+    include/osd.h): what Algorithm 1's buffer R needs of a target row.
+
+    ``logits`` is a [N,V] or [G,P,V] view with contiguous rows.  Outputs of rows with mask 0
+    are not written (pass a prefilled ``out`` to keep them).  ``rest=False`` skips the
+    log-mass; with ``out`` its ``rest`` says.
+    """
+    r = (_binding or _load_binding()).topk(logits, K, mask, temperature, rest, out, status, stream)
+    if r is not None:
+        return _native("osd_topk", r)
+    lib = load_library()
+    dev = _need_cuda(logits, mask, status, *(out or ()))
+    G, P, V, sg, sp = _rows_view(logits)
+    K = int(K)
+    lead = tuple(logits.shape[:-1])
+    if mask is not None and (mask.dtype != torch.uint8 or tuple(mask.shape) != lead or not mask.is_contiguous()):
+        raise ValueError("mask must be contiguous uint8 with the logits' leading shape")
+    dt = _dtype_code(logits)
+    if out is None:
+        if K < 1:
+            raise OsdError(OSD_ERR_INVALID_ARG, "osd_topk")
+        out = TopkResult(torch.empty(*lead, K, dtype=torch.float32, device=dev),
+                         torch.empty(*lead, K, dtype=torch.int32, device=dev),
+                         torch.empty(lead, dtype=torch.float32, device=dev) if rest else None)
+    for t, dtype, shape in ((out.values, torch.float32, lead + (K,)), (out.ids, torch.int32, lead + (K,)),
+                            (out.rest, torch.float32, lead)):
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError("out must hold contiguous float32 [.., K], int32 [.., K] and float32 [..] or None")
+    with _on(dev):
+        st = lib.osd_topk(_ptr(logits), dt, G, P, V, sg, sp, _ptr(mask), K, float(temperature), _ptr(out.values),
+                          _ptr(out.ids), _ptr(out.rest), _ptr(status), _stream(dev, stream))
+    if st != OSD_OK:
+        raise OsdError(st, "osd_topk")
     return out
 
 

@@ -27,6 +27,7 @@ namespace {
 PyObject* g_verify_result = nullptr;    // VerifyResult, DistillAcceptedResult, TreeResult
 PyObject* g_accepted_result = nullptr;
 PyObject* g_tree_result = nullptr;
+PyObject* g_topk_result = nullptr;      // TopkResult
 PyObject* g_cuda_stream = nullptr;      // "cuda_stream"
 
 // The arguments of one call: every tensor a plain CUDA tensor (no subclass, no
@@ -325,6 +326,60 @@ PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// logits, K, mask, temperature, rest, out, status, stream
+PyObject* topk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 8) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject* {
+        Call c;
+        const at::Tensor* x = c.tensor(a[0]);
+        Rows r;
+        if (!c.ok || !r.of(*x) || !PyLong_CheckExact(a[1])) Py_RETURN_NONE;
+        const int dt = dtype_code(*x);
+        const long K = PyLong_AsLong(a[1]);
+        if (K == -1 && PyErr_Occurred()) PyErr_Clear();
+        c.need(dt >= 0 && K >= 1 && K <= INT_MAX);
+        const at::Tensor *mask = c.optional(a[2]), *status = c.optional(a[6]);
+        const double temperature = c.number(a[3]);
+        const bool rest = a[4] == Py_True;
+        c.need(rest || a[4] == Py_False);
+        if (status) c.need(status->scalar_type() == at::kInt);
+        void* stream = c.stream(a[7]);
+        if (!c.ok) Py_RETURN_NONE;
+        const at::IntArrayRef lead = x->sizes().slice(0, x->dim() - 1);
+        at::DimVector top(lead.begin(), lead.end());
+        top.push_back(K);
+        if (mask) c.need(mask->scalar_type() == at::kByte && shaped(*mask, lead));
+        const at::Tensor* o[3] = {};
+        at::Tensor made[3];
+        const bool own = a[5] == Py_None;
+        if (!own) {
+            if (!c.need(Py_TYPE(a[5]) == reinterpret_cast<PyTypeObject*>(g_topk_result))) Py_RETURN_NONE;
+            for (int i = 0; i < 3; ++i) o[i] = c.member(a[5], i);
+            if (!c.need(c.ok && o[0] && o[1])) Py_RETURN_NONE;
+            c.need(o[0]->scalar_type() == at::kFloat && shaped(*o[0], top));
+            c.need(o[1]->scalar_type() == at::kInt && shaped(*o[1], top));
+            if (o[2]) c.need(o[2]->scalar_type() == at::kFloat && shaped(*o[2], lead));
+        }
+        if (!c.ok) Py_RETURN_NONE;
+        if (own) {
+            made[0] = fresh(top, at::kFloat, c.dev);
+            made[1] = fresh(top, at::kInt, c.dev);
+            if (rest) made[2] = fresh(lead, at::kFloat, c.dev);
+            for (int i = 0; i < 3; ++i) o[i] = made[i].defined() ? &made[i] : nullptr;
+        }
+        const void* xp = ptr(x);
+        const auto* mp = static_cast<const uint8_t*>(ptr(mask));
+        auto *vp = static_cast<float*>(ptr(o[0])), *rp = static_cast<float*>(ptr(o[2]));
+        auto *ip = static_cast<int32_t*>(ptr(o[1])), *sp = static_cast<int32_t*>(ptr(status));
+        const osd_status st = released([&]() {
+            return osd_topk(xp, osd_dtype(dt), int(r.G), int(r.P), int(r.V), r.sg, r.sp, mp, int(K), float(temperature), vp, ip,
+                            rp, sp, stream);
+        });
+        if (st != OSD_OK) return PyLong_FromLong(st);
+        return own ? result(g_topk_result, made, 3) : Py_NewRef(a[5]);
+    });
+}
+
 // draft, target, accepted, kind, beta, temperature, out, status, stream
 PyObject* distill_accepted(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 9) Py_RETURN_NONE;
@@ -480,15 +535,16 @@ PyObject* verify_tree(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     });
 }
 
-// VerifyResult, DistillAcceptedResult, TreeResult: the tuple classes the results come in
+// VerifyResult, DistillAcceptedResult, TreeResult, TopkResult: the tuple classes the results come in
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 3 || !PyType_Check(a[0]) || !PyType_Check(a[1]) || !PyType_Check(a[2])) {
-        PyErr_SetString(PyExc_TypeError, "setup takes the three result classes");
+    if (n != 4 || !PyType_Check(a[0]) || !PyType_Check(a[1]) || !PyType_Check(a[2]) || !PyType_Check(a[3])) {
+        PyErr_SetString(PyExc_TypeError, "setup takes the four result classes");
         return nullptr;
     }
     g_verify_result = Py_NewRef(a[0]);
     g_accepted_result = Py_NewRef(a[1]);
     g_tree_result = Py_NewRef(a[2]);
+    g_topk_result = Py_NewRef(a[3]);
     Py_RETURN_NONE;
 }
 
@@ -497,6 +553,7 @@ PyMethodDef methods[] = {{"setup", FAST(setup)},
                          {"verify", FAST(verify)},
                          {"verify_probs", FAST(verify_probs)},
                          {"distill", FAST(distill)},
+                         {"topk", FAST(topk)},
                          {"distill_accepted", FAST(distill_accepted)},
                          {"mixed_sample", FAST(mixed_sample)},
                          {"verify_tree", FAST(verify_tree)},

@@ -38,10 +38,32 @@ def test_verify_probs_refusals(osd):
     assert _verify_probs(osd, B=0, p=None, q=None, y=None, u=None, acc=None, out=None, mask=None) == osd.OSD_OK
 
 
+def _topk(osd, **kw):
+    a = dict(x=FAKE, dtype=0, G=2, P=1, V=16, sg=16, sp=0, mask=None, K=4, tau=1.0, values=FAKE, ids=FAKE, rest=None,
+             status=None, stream=None)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return osd.load_library().osd_topk(*a.values())
+
+
+def test_topk_refusals(osd):
+    bad, beyond = osd.OSD_ERR_INVALID_ARG, osd.OSD_ERR_UNSUPPORTED
+    for kw in ({"dtype": 2}, {"G": -1}, {"P": -1}, {"V": 0}, {"K": 0}, {"K": -3}, {"K": 17}, {"sg": -1}, {"sp": -1},
+               {"tau": 0.0}, {"tau": -1.0}, {"tau": float("nan")}, {"tau": float("inf")}, {"x": None}, {"values": None},
+               {"ids": None}, {"x": ODD}, {"x": ODD, "dtype": 1}, {"values": ODD}, {"ids": ODD}, {"rest": ODD}, {"status": ODD}):
+        assert _topk(osd, **kw) == bad, kw
+    assert _topk(osd, V=4000, K=osd.TOPK_MAX_K + 1) == beyond
+    assert _topk(osd, V=(1 << 21) + 1) == beyond
+    assert _topk(osd, G=1 << 20, P=1 << 20) == beyond
+    assert _topk(osd, G=0, x=None, values=None, ids=None) == osd.OSD_OK
+
+
 def test_python_takes_cuda_tensors_only(osd):
     p, y, u = torch.zeros(2, 3, 8), torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, 3)
     with pytest.raises(ValueError, match="CUDA tensors only"):
         osd.osd_verify_probs(None, p, y, u)
+    with pytest.raises(ValueError, match="CUDA tensors only"):
+        osd.osd_topk(p, 2)
 
 
 def test_version(osd):

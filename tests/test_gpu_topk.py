@@ -1,0 +1,216 @@
+"""osd_topk against the oracle: values and ids exactly, the log-mass of the rest within the
+rounding of an fp32 sum."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import compact
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+@pytest.fixture(scope="module")
+def osd():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA GPU")
+    import paper_2310_07177_gb300 as pkg
+    pkg.build_library()
+    pkg.load_library()
+    return pkg
+
+
+def _check_rest(got, ref, values, V, tau):
+    """The absolute error of log sum exp is the relative error of the sum: exponents a = x log2(e)/tau - M
+    with mass (|a| <= 40) rounded twice, 2 * 40 * 2^-24 * ln 2; ex2 2^-22; a sum of positive terms at
+    most V / 128 + 20 additions deep; and the result's own magnitude and the reference's, 4 roundings."""
+    fin = np.isfinite(ref)
+    np.testing.assert_array_equal(np.isfinite(got), fin)
+    np.testing.assert_array_equal(got[~fin], ref[~fin])
+    u = 2.0 ** -24
+    vk = values[:, -1]
+    big = np.abs(ref[fin]) + np.abs(vk[fin]) / tau
+    tol = 80 * u * 0.7 + 4 * u + (V / 128 + 20) * u + 4 * u * big
+    err = np.abs(got[fin] - ref[fin])
+    assert np.all(err <= tol), (err.max(), tol.min())
+
+
+def _check(osd, x, K, tau=1.0, **kw):
+    got = osd.osd_topk(x.cuda(), K, temperature=tau, **kw)
+    torch.cuda.synchronize()
+    v, i, r = compact.topk(x, K, tau)
+    np.testing.assert_array_equal(got.ids.cpu().numpy(), i)
+    np.testing.assert_array_equal(got.values.cpu().numpy().astype(np.float64), v)
+    _check_rest(got.rest.cpu().numpy().astype(np.float64), r, v, x.shape[1], tau)
+
+
+def _normal(N, V, dtype, seed, std=2.5):
+    return (torch.randn(N, V, generator=torch.Generator().manual_seed(seed)) * std).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [1, 2, 7, 33, 250, 1003, 1024, 4099, 9000])
+def test_sizes(osd, V, dtype):
+    for K in sorted({1, min(2, V), min(5, V), min(64, V), min(200, V), min(1000, V), min(1024, V)}):
+        _check(osd, _normal(5, V, dtype, V + K), K, 0.7)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,V,K", [(300, 32000, 64), (20, 32001, 33), (3, 128256, 256), (1, 160007, 1024), (2, 70000, 1),
+                                   (1, 600001, 512), (700, 3001, 16)])
+def test_large(osd, N, V, K, dtype):
+    _check(osd, _normal(N, V, dtype, N + V), K, 2.0 if K == 33 else 1.0)
+
+
+def _hard_rows(V, dtype):
+    """Rows on which a threshold from a part of the row, or a fixed room for candidates, fails."""
+    g = torch.Generator().manual_seed(3)
+    ramp = torch.arange(V).float() / 7
+    few = torch.full((V,), -INF)
+    few[torch.randperm(V, generator=g)[:9]] = torch.randn(9, generator=g)
+    one = torch.full((V,), -INF)
+    one[V // 2] = -1e30
+    late = torch.randn(V, generator=g)
+    late[-(V // 3):] += 50
+    stride = torch.randn(V, generator=g)
+    stride[::max(1, V // 40)] += 100  # the top entries at the same place of many tiles
+    block = torch.randn(V, generator=g)
+    block[V // 5:V // 5 + V // 6] += 200
+    signs = torch.zeros(V)
+    signs[::3] = -0.0
+    levels = torch.randint(0, 3, (V,), generator=g).float()
+    huge = torch.randn(V, generator=g) * 1e30
+    peak = torch.randn(V, generator=g) - 300
+    peak[V // 3] = 300
+    first = torch.zeros(V)
+    first[0] = 1
+    rows = [ramp, ramp.flip(0), few, one, late, stride, block, signs, levels, huge, peak, torch.full((V,), 3.0),
+            torch.full((V,), -INF), first, first.flip(0), torch.randn(V, generator=g) * 1e-3 + 5]
+    return torch.stack(rows).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,K", [(64, 13), (1000, 1), (5003, 100), (32000, 64), (32003, 1024), (128256, 300)])
+def test_hard_rows(osd, V, K, dtype):
+    _check(osd, _hard_rows(V, dtype), K)
+
+
+def test_scattered_maxima(osd):
+    """Many entries of equal value at random places: the lowest indices, whatever part found them."""
+    g = torch.Generator().manual_seed(4)
+    for V, K, hot in ((32000, 64, 100), (32000, 500, 501), (9001, 64, 3000), (128256, 1000, 5000)):
+        x = torch.randn(6, V, generator=g)
+        for r in range(6):
+            x[r, torch.randperm(V, generator=g)[:hot]] = 6.0
+        _check(osd, x, K)
+        _check(osd, x.bfloat16(), K)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_views_masks_and_given_outputs(osd, dtype):
+    """Rows of [B, k+1, V] off the 16-byte grid, positions first, a mask; inactive rows stay as they were."""
+    B, P, V, K = 7, 3, 1501, 40
+    x = _normal(B * P, V, dtype, 5).view(B, P, V)
+    wide = torch.zeros(P + 1, B, V + 4, dtype=dtype, device="cuda")
+    wide[:P, :, 3:V + 3] = x.transpose(0, 1).cuda()
+    view = wide[:P, :, 3:V + 3].transpose(0, 1)
+    mask = (torch.arange(B * P) % 3 != 1).to(torch.uint8).view(B, P)
+    out = osd.TopkResult(torch.full((B, P, K), 7.0, device="cuda"), torch.full((B, P, K), 7, dtype=torch.int32, device="cuda"),
+                         torch.full((B, P), 7.0, device="cuda"))
+    status = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+    got = osd.osd_topk(view, K, mask.cuda(), out=out, status=status)
+    assert got is out and status.item() == 0
+    v, i, r = (a.reshape((B, P) + a.shape[1:]) for a in compact.topk(x.view(-1, V), K))
+    on = mask.bool().numpy()
+    np.testing.assert_array_equal(out.ids.cpu().numpy()[on], i[on])
+    np.testing.assert_array_equal(out.values.cpu().numpy()[on], v[on])
+    _check_rest(out.rest.cpu().numpy()[on].astype(np.float64), r[on], v[on], V, 1.0)
+    for t in out:
+        assert (t.cpu().numpy()[~on] == 7).all()
+    bare = osd.osd_topk(view, K, rest=False)
+    assert bare.rest is None and np.array_equal(bare.ids.cpu().numpy(), i)
+    one = osd.osd_topk(x[:1, 0].cuda().expand(5, V), K)  # one row five times
+    np.testing.assert_array_equal(one.ids.cpu().numpy(), np.broadcast_to(i[0, 0], (5, K)))
+    none = osd.osd_topk(x[:0, 0].cuda(), K)
+    assert none.values.shape == (0, K) and none.rest.shape == (0,)
+    empty = osd.osd_topk(view, K, torch.zeros_like(mask).cuda(), out=out)
+    assert (empty.ids.cpu().numpy()[~on] == 7).all()
+
+
+def test_offsets_past_32_bits(osd):
+    V, far = 2000, (1 << 31) + 8 * 13
+    x = _normal(2, V, torch.bfloat16, 6)
+    view = torch.zeros(far + V, dtype=torch.bfloat16, device="cuda").as_strided((2, V), (far, 1))
+    view.copy_(x.cuda())
+    got = osd.osd_topk(view, 50)
+    np.testing.assert_array_equal(got.ids.cpu().numpy(), compact.topk(x, 50)[1])
+
+
+def test_outside_the_domain_ends_in_range(osd):
+    """NaN and +inf: unspecified entries, but ids in [-1, V) and no fault."""
+    V = 5000
+    x = _normal(6, V, torch.float32, 7).cuda()
+    x[0, ::2] = float("nan")
+    x[1] = float("nan")
+    x[2, 17] = INF
+    x[3] = INF
+    x[4, ::3] = -float("nan")
+    for t in (x, x.bfloat16()):
+        for K in (1, 64, 1000):
+            got = osd.osd_topk(t, K)
+            torch.cuda.synchronize()
+            assert ((got.ids >= -1) & (got.ids < V)).all()
+            np.testing.assert_array_equal(got.ids[5].cpu().numpy(), compact.topk(t[5:], K)[1][0])
+
+
+def test_graph_and_streams(osd):
+    a, b = _normal(40, 32000, torch.bfloat16, 8), _normal(40, 32000, torch.bfloat16, 9)
+    static = a.cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        osd.osd_topk(static, 64)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        res = osd.osd_topk(static, 64)
+    for x in (b, a):
+        static.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(res.ids.cpu().numpy(), compact.topk(x, 64)[1])
+    side.wait_stream(torch.cuda.current_stream())
+    two = osd.osd_topk(static, 64, stream=side)
+    one = osd.osd_topk(b.cuda(), 64)
+    torch.cuda.synchronize()
+    assert torch.equal(two.ids, res.ids) and torch.equal(two.rest, res.rest)
+    np.testing.assert_array_equal(one.ids.cpu().numpy(), compact.topk(b, 64)[1])
+
+
+def test_native_equals_ctypes_and_refusals(osd, monkeypatch):
+    x = _normal(6, 900, torch.bfloat16, 10).cuda()
+    a = osd.osd_topk(x, 20, temperature=2)
+    real = osd._binding
+    assert real.topk(x, 20, None, 1.0, True, None, None, None) is not None
+
+    class Nothing:
+        def __getattr__(self, name):
+            return lambda *args: None
+    monkeypatch.setattr(osd, "_binding", Nothing())
+    b = osd.osd_topk(x, 20, temperature=2)
+    for s, t in zip(a, b):
+        assert s.dtype == t.dtype and torch.equal(s, t)
+    monkeypatch.setattr(osd, "_binding", real)
+    for K in (0, -1, 901, 1025):
+        with pytest.raises(osd.OsdError):
+            osd.osd_topk(x, K)
+    with pytest.raises(osd.OsdError):
+        osd.osd_topk(x, 5, temperature=0.0)
+    with pytest.raises(ValueError, match="mask"):
+        osd.osd_topk(x, 5, torch.ones(6, device="cuda"))
+    with pytest.raises(ValueError, match="out must"):
+        osd.osd_topk(x, 5, out=a)
+    with pytest.raises(ValueError, match="contiguous"):
+        osd.osd_topk(x.t(), 5)
+    with pytest.raises(TypeError, match="float32 or bfloat16"):
+        osd.osd_topk(x.half(), 5)

@@ -83,3 +83,23 @@ def test_agrees_with_verification_from_logits(T):
     assert np.array_equal(acc[clear], ref["accepted"][clear])
     assert np.array_equal(out[clear], ref["out_tokens"][clear])
     assert np.array_equal(mask[clear], ref["mismatch_mask"][clear])
+
+
+# ------------------------------------------------------------------ top logits
+def test_worked_topk():
+    x = np.float32([[1, 3, 3, -np.inf, 0, 3, -0.0], [-np.inf, -np.inf, 2, -np.inf, -np.inf, -np.inf, -np.inf]])
+    v, i, r = compact.topk(x, 4, 0.5)
+    assert i.tolist() == [[1, 2, 5, 0], [2, 0, 1, 3]]
+    assert v.tolist() == [[3, 3, 3, 1], [2, -np.inf, -np.inf, -np.inf]]
+    assert r[0] == pytest.approx(np.log(2.0)) and r[1] == -np.inf
+    assert compact.topk(x, 7)[2].tolist() == [-np.inf, -np.inf]
+
+
+def test_topk_and_its_rest_make_up_the_row():
+    rng = np.random.default_rng(2)
+    x = rng.normal(size=(50, 301)) * 4
+    for tau in (0.5, 1.0, 2.0):
+        v, i, r = compact.topk(x, 20, tau)
+        total = np.logaddexp(np.log(np.exp(v / tau).sum(1)), r)
+        np.testing.assert_allclose(total, np.log(np.exp(x / tau).sum(1)), rtol=1e-13)
+        assert (np.diff(v, axis=1) <= 0).all() and np.array_equal(np.sort(x, axis=1)[:, ::-1][:, :20], v)
