@@ -25,6 +25,7 @@
  *                different lengths and drafts without a distribution.
  *   osd_topk     the top logits of target rows and the log of the mass of the
  *                rest: the compact form in which buffer R keeps a row.
+ *   osd_distill_topk  osd_distill against such compact target rows.
  *
  * Conventions shared by every entry point:
  *   - All array arguments are DEVICE pointers to caller-owned memory on the
@@ -88,7 +89,7 @@ const char *osd_status_string(osd_status status);
  * osd_distill_accepted; 2.2 added osd_mixed_sample; 2.3 added
  * osd_verify_tree; 2.4 added osd_check_bounded_wait; 2.5 raised
  * osd_mixed_sample's vocabulary limit to OSD_VERIFY_MAX_V; 2.6 added
- * osd_verify_probs and osd_topk. */
+ * osd_verify_probs, osd_topk and osd_distill_topk. */
 int osd_abi_version(void);
 
 /*
@@ -381,6 +382,41 @@ osd_status osd_verify_probs(const void *draft_probs, const void *target_probs, o
 osd_status osd_topk(const void *logits, osd_dtype dtype, int G, int P, int V, int64_t stride_g,
                     int64_t stride_p, const uint8_t *mask, int K, float temperature, float *values,
                     int32_t *ids, float *rest, int32_t *status, void *stream);
+
+/*
+ * Per-position distillation loss and gradient (Eq. 2-3) against compact target
+ * rows: the top entries that osd_topk kept of each, or any others.  Target and
+ * draft are compared on the K kept tokens and, as one more class, all other
+ * tokens together: with c over these classes and tau = `temperature`
+ *   p_c  from exp(value_c / tau) and exp(rest), normalised over the classes
+ *        (without `rest` the other tokens have target probability 0),
+ *   q_c  the mass of softmax(draft row / tau) in class c,
+ * the loss is osd_distill's D(p || q) over the classes.  OSD_CE's label is the
+ * token of the largest value (lowest id on ties); it does not read `rest`.
+ * dlogits is the gradient with respect to every draft logit: the others share
+ * their class's derivative, each by its own probability.
+ *
+ * draft_logits   rows laid out as in osd_distill
+ * values, ids    [G, P, K] fp32 and int32, contiguous, in any order.  A negative
+ *                id marks an unused entry.  An id >= V, or one that occurs twice
+ *                in a row, makes the row bad: loss NaN, gradient 0, and *status
+ *                OSD_ERR_INVALID_ARG.
+ * rest           [G, P] fp32, nullable: osd_topk's, taken at the same temperature
+ * mask, kind, beta, temperature, loss, dlogits, status  as in osd_distill
+ * A row without target mass (all ids negative or values -inf, no rest; for
+ * OSD_CE without a label) has loss 0 and gradient 0.  OSD_RKL's loss is +inf,
+ * and its gradient 0, where the draft has mass in a class without target mass:
+ * without `rest` the call is refused unless K >= V.  OSD_FKL's is +inf where the
+ * target has mass in a class without draft mass; its gradient is q - p all the
+ * same.  Values and draft logits of +inf or NaN, a rest of +inf or NaN, and
+ * draft rows of -inf only are outside the domain: results are unspecified.
+ * Limits: 1 <= K <= OSD_TOPK_MAX_K, V <= 393216, strides >= 0.  No workspace.
+ */
+osd_status osd_distill_topk(const void *draft_logits, osd_dtype dtype, int G, int P, int V,
+                            int64_t d_stride_g, int64_t d_stride_p, const float *values,
+                            const int32_t *ids, const float *rest, int K, const uint8_t *mask,
+                            osd_loss kind, float beta, float temperature, float *loss,
+                            float *dlogits, int32_t *status, void *stream);
 
 /*
  * Mixed-token sampling (Section 4.1): one token per position from the mixture

@@ -77,3 +77,74 @@ def topk(logits, K, temperature=1.0):
         if o.size and o[0] > -np.inf:  # o[0] is the largest of them
             rest[n] = o[0] + np.log(np.exp(o - o[0]).sum())
     return values, top.astype(np.int32), rest
+
+
+def _kl(a, b):
+    """sum a log(a / b) over the classes where a > 0 (+inf where b = 0 there)."""
+    on = a > 0
+    with np.errstate(divide="ignore"):
+        return float((a[on] * (np.log(a[on]) - np.log(b[on]))).sum())
+
+
+def distill_topk_row(z, values, ids, rest, kind, beta=0.5, tau=1.0):
+    """osd_distill_topk of one row: (loss, gradient, the target's share of every entry, q), the
+    share being p_c of a kept token and p_R q_j / q_R of another."""
+    z, values, ids = _f64(z), _f64(values), np.asarray(ids, np.int64)
+    V = len(z)
+    used = ids >= 0
+    values, ids = values[used], ids[used]
+    nothing = np.zeros(V), np.zeros(V), np.zeros(V)
+    if np.any(ids >= V) or len(np.unique(ids)) != len(ids):
+        return (np.nan,) + nothing
+    rest = -np.inf if rest is None or kind == "ce" else float(rest)
+    t = np.concatenate([values / tau, [rest]])
+    if not t.size or t.max() == -np.inf:
+        return (0.0,) + nothing
+    e = np.exp(t - t.max())
+    p = e / e.sum()
+    if kind == "ce":
+        best = ids[values == values.max()].min()
+        p = np.concatenate([(ids == best).astype(np.float64), [0.0]])
+    x = np.exp(z / tau - z.max() / tau)
+    x /= x.sum()
+    other = np.ones(V, bool)
+    other[ids] = False
+    q = np.concatenate([x[ids], [x[other].sum()]])
+    # g = dl/dq_c: 0 stands in where q_c = 0, whose product with q_c is 0
+    on = q > 0
+    g = np.zeros_like(q)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        if kind in ("fkl", "ce"):
+            loss = _kl(p, q)
+            g[on] = -p[on] / q[on]
+        elif kind == "rkl":
+            loss = _kl(q, p)
+            if loss == np.inf:
+                return loss, np.zeros(V), np.zeros(V), x
+            g[on] = np.log(q[on] / p[on])
+        elif kind == "jsd":
+            m = beta * p + (1 - beta) * q
+            loss = (beta * _kl(p, m) if beta > 0 else 0.0) + ((1 - beta) * _kl(q, m) if beta < 1 else 0.0)
+            if beta < 1:
+                g[on] = (1 - beta) * np.log(q[on] / m[on])
+        else:
+            loss = 0.5 * np.abs(p - q).sum()
+            g = 0.5 * np.sign(q - p)
+    g = g - (q * g).sum()
+    grad, share = x * g[-1], np.zeros(V)
+    grad[ids] = q[:-1] * g[:-1]
+    if kind in ("fkl", "ce"):  # q - p, also where q_c = 0
+        grad[ids] = q[:-1] - p[:-1]
+        grad[other] = x[other] - (p[-1] * x[other] / q[-1] if q[-1] > 0 else 0.0)
+    share[ids] = p[:-1]
+    if q[-1] > 0:
+        share[other] = p[-1] * x[other] / q[-1]
+    return float(loss), grad / tau, share, x
+
+
+def distill_topk(z, values, ids, rest, kind, beta=0.5, tau=1.0):
+    """Rows [N, V]: (loss [N], gradient, share, q [N, V])."""
+    z, values, ids, rest = _f64(z), _f64(values), np.asarray(ids, np.int64), _f64(rest)
+    rows = [distill_topk_row(z[n], values[n], ids[n], None if rest is None else rest[n], kind, beta, tau)
+            for n in range(len(z))]
+    return tuple(np.array(c) for c in zip(*rows))

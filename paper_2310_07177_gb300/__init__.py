@@ -37,7 +37,7 @@ TOPK_MAX_K = 1024
 # every symbol include/osd.h declares
 EXPORTS = ("osd_status_string", "osd_abi_version", "osd_verify_workspace_size",
            "osd_verify", "osd_verify_noalloc", "osd_distill", "osd_distill_accepted",
-           "osd_verify_probs", "osd_topk", "osd_mixed_sample", "osd_verify_tree_workspace_size", "osd_verify_tree", "osd_check_bounded_wait")
+           "osd_verify_probs", "osd_topk", "osd_distill_topk", "osd_mixed_sample", "osd_verify_tree_workspace_size", "osd_verify_tree", "osd_check_bounded_wait")
 
 
 class OsdError(RuntimeError):
@@ -85,6 +85,8 @@ def load_library():
     lib.osd_verify_probs.argtypes = [vp, vp, i32, i32, i32, i32, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp]
     lib.osd_topk.restype = i32
     lib.osd_topk.argtypes = [vp, i32, i32, i32, i32, i64, i64, vp, i32, f32, vp, vp, vp, vp, vp]
+    lib.osd_distill_topk.restype = i32
+    lib.osd_distill_topk.argtypes = [vp, i32, i32, i32, i32, i64, i64, vp, vp, vp, i32, vp, i32, f32, f32, vp, vp, vp, vp]
     lib.osd_check_bounded_wait.restype = i32
     lib.osd_check_bounded_wait.argtypes = [ctypes.c_uint32, vp, vp, vp]
     lib.osd_mixed_sample.restype = i32
@@ -103,7 +105,7 @@ class _NoBinding:
     def _none(*args):
         return None
 
-    verify = verify_probs = distill = distill_accepted = mixed_sample = verify_tree = topk = _none
+    verify = verify_probs = distill = distill_accepted = mixed_sample = verify_tree = topk = distill_topk = _none
 
 
 def _load_binding():
@@ -466,6 +468,55 @@ def osd_topk(logits: torch.Tensor, K: int, mask: Optional[torch.Tensor] = None, 
     if st != OSD_OK:
         raise OsdError(st, "osd_topk")
     return out
+
+
+def osd_distill_topk(draft_logits: torch.Tensor, top: TopkResult, mask: Optional[torch.Tensor] = None,
+                     loss_kind: str = "fkl", beta: float = 0.5, *, temperature: float = 1.0,
+                     loss: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
+                     status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Per-position distillation loss and gradient (Eq. 2-3) against compact target rows:
+    the kept tokens and all others together as one more class (see include/osd.h).
+
+    ``top`` is osd_topk's result for these rows at the same ``temperature``, or any tuple
+    ``(values [.., K] fp32, ids [.., K] int32, rest [..] fp32 or None)``; negative ids are
+    unused entries.  The other arguments and the results are osd_distill's.
+    """
+    r = (_binding or _load_binding()).distill_topk(draft_logits, top, mask, loss_kind, beta, temperature, loss, dlogits,
+                                                   status, stream)
+    if r is not None:
+        return _native("osd_distill_topk", r)
+    lib = load_library()
+    values, ids, rest = top
+    dev = _need_cuda(draft_logits, values, ids, rest, mask, loss, dlogits, status)
+    G, P, V, dsg, dsp = _rows_view(draft_logits)
+    lead = tuple(draft_logits.shape[:-1])
+    K = values.shape[-1]
+    if (values.dtype != torch.float32 or ids.dtype != torch.int32 or tuple(values.shape) != lead + (K,)
+            or tuple(ids.shape) != lead + (K,) or not values.is_contiguous() or not ids.is_contiguous()):
+        raise ValueError("top must hold contiguous float32 values and int32 ids [.., K] with the logits' leading shape")
+    if rest is not None and (rest.dtype != torch.float32 or tuple(rest.shape) != lead or not rest.is_contiguous()):
+        raise ValueError("rest must be contiguous float32 with the logits' leading shape")
+    if mask is not None and (mask.dtype != torch.uint8 or tuple(mask.shape) != lead or not mask.is_contiguous()):
+        raise ValueError("mask must be contiguous uint8 with the logits' leading shape")
+    if status is not None and status.dtype != torch.int32:
+        raise ValueError("status must be int32")
+    dt = _dtype_code(draft_logits)
+    if loss is None:
+        loss = torch.empty(lead, dtype=torch.float32, device=dev)
+    if dlogits is None:
+        dlogits = torch.empty(*lead, V, dtype=torch.float32, device=dev)
+    if (loss.dtype != torch.float32 or not loss.is_contiguous() or tuple(loss.shape) != lead
+            or dlogits.dtype != torch.float32 or not dlogits.is_contiguous()
+            or tuple(dlogits.shape) != lead + (V,)):
+        raise ValueError("loss / dlogits must be contiguous float32 of the logits' shape")
+    kind = LOSS_KINDS[loss_kind] if isinstance(loss_kind, str) else int(loss_kind)
+    with _on(dev):
+        st = lib.osd_distill_topk(_ptr(draft_logits), dt, G, P, V, dsg, dsp, _ptr(values), _ptr(ids), _ptr(rest), K,
+                                  _ptr(mask), kind, float(beta), float(temperature), _ptr(loss), _ptr(dlogits),
+                                  _ptr(status), _stream(dev, stream))
+    if st != OSD_OK:
+        raise OsdError(st, "osd_distill_topk")
+    return loss, dlogits
 
 
 def _rows_2d(t: torch.Tensor):

@@ -380,6 +380,57 @@ PyObject* topk(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// draft, top, mask, kind, beta, temperature, loss, dlogits, status, stream
+PyObject* distill_topk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 10) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject* {
+        Call c;
+        const at::Tensor* draft = c.tensor(a[0]);
+        Rows d;
+        if (!c.ok || !d.of(*draft) || !PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[1]) != 3) Py_RETURN_NONE;
+        const int dt = dtype_code(*draft);
+        const at::Tensor *values = c.tensor(PyTuple_GET_ITEM(a[1], 0)), *ids = c.tensor(PyTuple_GET_ITEM(a[1], 1)),
+                         *rest = c.optional(PyTuple_GET_ITEM(a[1], 2)), *mask = c.optional(a[2]), *loss = c.optional(a[6]),
+                         *dlogits = c.optional(a[7]), *status = c.optional(a[8]);
+        const int kind = c.kind(a[3]);
+        const double beta = c.number(a[4]), temperature = c.number(a[5]);
+        void* stream = c.stream(a[9]);
+        if (!c.need(c.ok && dt >= 0 && values->dim() == draft->dim())) Py_RETURN_NONE;
+        const at::IntArrayRef full = draft->sizes(), lead = full.slice(0, full.size() - 1);
+        at::DimVector top(lead.begin(), lead.end());
+        top.push_back(values->size(-1));
+        c.need(values->scalar_type() == at::kFloat && shaped(*values, top));
+        c.need(ids->scalar_type() == at::kInt && shaped(*ids, top));
+        if (rest) c.need(rest->scalar_type() == at::kFloat && shaped(*rest, lead));
+        if (mask) c.need(mask->scalar_type() == at::kByte && shaped(*mask, lead));
+        if (loss) c.need(loss->scalar_type() == at::kFloat && shaped(*loss, lead));
+        if (dlogits) c.need(dlogits->scalar_type() == at::kFloat && shaped(*dlogits, full));
+        if (status) c.need(status->scalar_type() == at::kInt);
+        if (!c.ok) Py_RETURN_NONE;
+        at::Tensor made[2];
+        if (!loss) loss = &(made[0] = fresh(lead, at::kFloat, c.dev));
+        if (!dlogits) dlogits = &(made[1] = fresh(full, at::kFloat, c.dev));
+        const void* zp = ptr(draft);
+        const auto *vp = static_cast<const float*>(ptr(values)), *rp = static_cast<const float*>(ptr(rest));
+        const auto* ip = static_cast<const int32_t*>(ptr(ids));
+        const auto* mp = static_cast<const uint8_t*>(ptr(mask));
+        auto *lp = static_cast<float*>(ptr(loss)), *gp = static_cast<float*>(ptr(dlogits));
+        auto* sp = static_cast<int32_t*>(ptr(status));
+        const int K = int(top.back());
+        const osd_status st = released([&]() {
+            return osd_distill_topk(zp, osd_dtype(dt), int(d.G), int(d.P), int(d.V), d.sg, d.sp, vp, ip, rp, K, mp,
+                                    osd_loss(kind), float(beta), float(temperature), lp, gp, sp, stream);
+        });
+        if (st != OSD_OK) return PyLong_FromLong(st);
+        PyObject* l = made[0].defined() ? THPVariable_Wrap(made[0]) : Py_NewRef(a[6]);
+        PyObject* g = made[1].defined() ? THPVariable_Wrap(made[1]) : Py_NewRef(a[7]);
+        PyObject* r = (l && g) ? PyTuple_Pack(2, l, g) : nullptr;
+        Py_XDECREF(l);
+        Py_XDECREF(g);
+        return r;
+    });
+}
+
 // draft, target, accepted, kind, beta, temperature, out, status, stream
 PyObject* distill_accepted(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 9) Py_RETURN_NONE;
@@ -554,6 +605,7 @@ PyMethodDef methods[] = {{"setup", FAST(setup)},
                          {"verify_probs", FAST(verify_probs)},
                          {"distill", FAST(distill)},
                          {"topk", FAST(topk)},
+                         {"distill_topk", FAST(distill_topk)},
                          {"distill_accepted", FAST(distill_accepted)},
                          {"mixed_sample", FAST(mixed_sample)},
                          {"verify_tree", FAST(verify_tree)},

@@ -58,12 +58,36 @@ def test_topk_refusals(osd):
     assert _topk(osd, G=0, x=None, values=None, ids=None) == osd.OSD_OK
 
 
+def _distill_topk(osd, **kw):
+    a = dict(z=FAKE, dtype=0, G=2, P=1, V=16, sg=16, sp=0, values=FAKE, ids=FAKE, rest=FAKE, K=4, mask=None, kind=0, beta=0.5,
+             tau=1.0, loss=FAKE, dlogits=FAKE, status=None, stream=None)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return osd.load_library().osd_distill_topk(*a.values())
+
+
+def test_distill_topk_refusals(osd):
+    bad, beyond = osd.OSD_ERR_INVALID_ARG, osd.OSD_ERR_UNSUPPORTED
+    for kw in ({"dtype": 2}, {"G": -1}, {"P": -1}, {"V": 0}, {"K": 0}, {"sg": -1}, {"sp": -1}, {"kind": 5}, {"kind": -1},
+               {"tau": 0.0}, {"tau": -1.0}, {"tau": float("nan")}, {"tau": float("inf")}, {"kind": 2, "beta": 1.5},
+               {"kind": 2, "beta": float("nan")}, {"kind": 1, "rest": None}, {"z": None}, {"values": None}, {"ids": None},
+               {"loss": None}, {"dlogits": None}, {"z": ODD}, {"z": ODD, "dtype": 1}, {"values": ODD}, {"ids": ODD},
+               {"rest": ODD}, {"loss": ODD}, {"dlogits": ODD}, {"status": ODD}):
+        assert _distill_topk(osd, **kw) == bad, kw
+    assert _distill_topk(osd, K=osd.TOPK_MAX_K + 1) == beyond
+    assert _distill_topk(osd, V=400000) == beyond
+    assert _distill_topk(osd, G=1 << 20, P=1 << 20) == beyond
+    assert _distill_topk(osd, G=0, z=None, values=None, ids=None, rest=None, loss=None, dlogits=None) == osd.OSD_OK
+
+
 def test_python_takes_cuda_tensors_only(osd):
     p, y, u = torch.zeros(2, 3, 8), torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, 3)
     with pytest.raises(ValueError, match="CUDA tensors only"):
         osd.osd_verify_probs(None, p, y, u)
     with pytest.raises(ValueError, match="CUDA tensors only"):
         osd.osd_topk(p, 2)
+    with pytest.raises(ValueError, match="CUDA tensors only"):
+        osd.osd_distill_topk(p, (p, p.int(), None))
 
 
 def test_version(osd):

@@ -1,0 +1,367 @@
+"""osd_distill_topk against the oracle, and the three operations on compact targets run as
+one step: verification, the rejected rows kept, distillation from them."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import compact
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+KINDS = ["fkl", "rkl", "jsd", "tvd", "ce"]
+
+
+@pytest.fixture(scope="module")
+def osd():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA GPU")
+    import paper_2310_07177_gb300 as pkg
+    pkg.build_library()
+    pkg.load_library()
+    return pkg
+
+
+# Exponents of entries with mass, |a| <= 40 in base 2, carry three roundings of 2^-24 |a| (their difference, the
+# constant, the product): a relative error of 40 * 3 * 2^-24 * ln 2 = 5e-6 of p and q; ex2, log2 and the sums
+# (positive terms, at most V / 128 + 20 additions deep, their errors of either sign) add about as much.
+REL = 2e-5
+
+
+def _compare(loss, grad, z, top, kind, beta, tau, rows=None):
+    v, i, r = top
+    ref_l, ref_g, share, q = compact.distill_topk(z, v, i, r, kind, beta, tau)
+    loss, grad = loss.cpu().double().numpy(), grad.cpu().double().numpy()
+    fin = np.isfinite(ref_l)
+    np.testing.assert_array_equal(loss[~fin], ref_l[~fin])
+    assert np.all(np.abs(loss[fin] - ref_l[fin]) <= REL * np.abs(ref_l[fin]) + REL), np.abs(loss - ref_l)[fin].max()
+    use = np.ones(len(ref_l), bool)
+    if kind == "tvd":  # a class where p and q are equal within rounding may take either sign: rows without one
+        use = _clear_of_ties(z, v, i, r, tau)
+    # |dl/dz_j| is made of q_j times a factor, and of the target's share where the two are subtracted; the floor:
+    # fp32 products below 2^-126 flush to zero
+    tol = REL * (np.abs(ref_g) + (q + share) / tau) + 2e-38
+    err = np.abs(grad - ref_g)
+    bad = (err > tol) & use[:, None]
+    assert not bad.any(), (np.argwhere(bad)[:5], err[bad][:5], ref_g[bad][:5])
+    return use.sum()
+
+
+def _clear_of_ties(z, v, i, r, tau):
+    z, v, i = z.double().numpy() / tau, v.double().numpy() / tau, i.numpy()
+    r = np.full(len(z), -INF) if r is None else r.double().numpy()
+    ok = np.ones(len(z), bool)
+    for n in range(len(z)):
+        used = i[n] >= 0
+        t = np.concatenate([v[n][used], [r[n]]])
+        x = np.exp(z[n] - z[n].max())
+        other = np.ones(len(x), bool)
+        other[i[n][used]] = False
+        q = np.concatenate([x[i[n][used]], [x[other].sum()]]) / x.sum()
+        p = np.exp(t - t.max())
+        p /= p.sum()
+        ok[n] = np.all(np.abs(q - p) > 1e-4 * np.maximum(p, q)) or not np.any(q + p)
+    return ok
+
+
+def _inputs(N, V, K, dtype, seed, tau=1.0, rest=True, noise=1.5):
+    g = torch.Generator().manual_seed(seed)
+    z = (torch.randn(N, V, generator=g) * 2).to(dtype)
+    t = z.float() + torch.randn(N, V, generator=g) * noise
+    v, i, r = compact.topk(t, K, tau)
+    return z, (torch.tensor(v).float(), torch.tensor(i), torch.tensor(r).float() if rest else None)
+
+
+def _cuda(top):
+    return tuple(None if t is None else t.cuda() for t in top)
+
+
+def _check(osd, z, top, kind, beta=0.5, tau=1.0, **kw):
+    status = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+    loss, grad = osd.osd_distill_topk(z.cuda(), _cuda(top), None, kind, beta, temperature=tau, status=status, **kw)
+    torch.cuda.synchronize()
+    assert status.item() == 0
+    return _compare(loss, grad, z, top, kind, beta, tau)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_small(osd, kind, dtype):
+    for V in (1, 2, 7, 33, 250, 1003, 4099):
+        for K in sorted({1, min(2, V), min(5, V), min(64, V), min(300, V), V if V < 1024 else 1024}):
+            z, top = _inputs(5, V, K, dtype, V + K, 0.7)
+            if kind == "rkl" and K == V:
+                top = top[:2] + (None,)  # every token kept: nothing else to hold mass
+            _check(osd, z, top, kind, 0.3, 0.7)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,V,K", [(40, 32000, 64), (6, 32001, 100), (2, 128256, 256), (1, 160007, 1024), (400, 2999, 8),
+                                   (3, 393216, 17)])
+def test_large(osd, N, V, K, dtype, kind):
+    z, top = _inputs(N, V, K, dtype, N + V, 2.0)
+    used = _check(osd, z, top, kind, 0.5, 2.0)
+    assert used > 0 or K > 200
+    if kind != "rkl":  # a teacher cut to its kept tokens
+        _check(osd, z, top[:2] + (None,), kind, 0.1, 2.0)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_unused_entries_any_order_and_masked_vocabulary(osd, kind, dtype):
+    """Kept tokens in random order, some ids unused, part of the draft's vocabulary at -inf, and
+    values of -inf among the kept."""
+    N, V, K = 12, 3001, 40
+    g = torch.Generator().manual_seed(11)
+    z, (v, i, r) = _inputs(N, V, K, dtype, 12)
+    z[:, 2000:2100] = -INF  # a forbidden range of the draft's
+    perm = torch.stack([torch.randperm(K, generator=g) for _ in range(N)])
+    v, i = v.gather(1, perm), i.gather(1, perm.to(torch.int64)).clone()
+    inside = (i >= 2000) & (i < 2100)
+    i[inside] = -5  # (a kept token without draft mass has its own test)
+    i[torch.rand(N, K, generator=g) < 0.3] = -1
+    if kind not in ("rkl", "ce"):
+        v = torch.where(torch.rand(N, K, generator=g) < 0.1, -INF, v)
+    _check(osd, z, (v, i, r), kind)
+
+
+def test_rows_without_target_mass(osd):
+    z, (v, i, r) = _inputs(5, 700, 6, torch.float32, 13)
+    i[0], r[0] = -1, -INF       # nothing
+    v[1], r[1] = -INF, -INF     # kept tokens without mass
+    i[2] = -1                   # only the others have mass: p = q there
+    r[3] = -INF
+    for kind in KINDS:
+        if kind == "rkl":
+            r[3] = 0.0
+        _check(osd, z, (v, i, r), kind)
+        loss, grad = osd.osd_distill_topk(z.cuda(), _cuda((v, i, r)), None, kind)
+        assert (loss[:2] == 0).all() and (grad[:2] == 0).all()
+
+
+def test_infinite_losses(osd):
+    """FKL: a kept token with target mass and draft logit -inf: +inf, gradient q - p.  RKL: draft mass
+    where the target has none: +inf, gradient 0.  JSD and TVD stay finite."""
+    z, (v, i, r) = _inputs(4, 900, 6, torch.bfloat16, 14)
+    z[0, i[0, 2].item()] = -INF
+    v[1, 3] = -INF
+    r[2] = -INF
+    for kind in KINDS:
+        loss, grad = osd.osd_distill_topk(z.cuda(), _cuda((v, i, r)), None, kind)
+        _compare(loss, grad, z, (v, i, r), kind, 0.5, 1.0)
+        want = {"fkl": [True, False, False, False], "rkl": [False, True, True, False]}.get(kind, [False] * 4)
+        assert torch.isposinf(loss).tolist() == want
+        assert torch.isfinite(grad).all()
+
+
+def test_bad_rows(osd):
+    """Ids past the vocabulary and repeated ids: loss NaN, gradient 0, status; the other rows are right."""
+    for V, K, csizes in ((900, 8, 1), (40000, 200, 1), (128256, 64, 1)):
+        z, (v, i, r) = _inputs(5, V, K, torch.bfloat16, V)
+        good = i.clone()
+        i[0, 3], i[1, 5], i[3, 0] = V, i[1, 2], 1 << 30
+        i[4, K - 1] = i[4, 0]
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        dl = torch.full((5, V), 7.0, device="cuda")
+        loss, grad = osd.osd_distill_topk(z.cuda(), _cuda((v, i, r)), None, "jsd", status=status, dlogits=dl)
+        assert status.item() == osd.OSD_ERR_INVALID_ARG
+        assert torch.isnan(loss).tolist() == [True, True, False, True, True]
+        assert (grad[[0, 1, 3, 4]] == 0).all()
+        _compare(loss[2:3], grad[2:3], z[2:3], (v[2:3], good[2:3], r[2:3]), "jsd", 0.5, 1.0)
+
+
+def test_far_logits(osd):
+    """Kept tokens hundreds above or below the others: the others' mass is summed against their own
+    maximum, and the log-masses stay finite."""
+    V, K = 2000, 8
+    g = torch.Generator().manual_seed(15)
+    z = torch.randn(4, V, generator=g)
+    i = torch.stack([torch.randperm(V, generator=g)[:K] for _ in range(4)]).int()
+    v = torch.randn(4, K, generator=g)
+    r = torch.randn(4, generator=g)
+    z[0, i[0].long()] += 300
+    z[1, i[1].long()] -= 300
+    v[2] += 200
+    r[3] += 200
+    for kind in ("fkl", "rkl", "jsd", "ce"):
+        loss, grad = osd.osd_distill_topk(z.cuda(), _cuda((v, i, r)), None, kind)
+        ref_l, ref_g, _, _ = compact.distill_topk(z, v, i, r, kind)
+        np.testing.assert_allclose(loss.cpu().numpy(), ref_l, rtol=1e-5, atol=1e-5)
+        np.testing.assert_allclose(grad.cpu().numpy(), ref_g, rtol=1e-4, atol=1e-6)
+
+
+def test_identical_rows(osd):
+    """A teacher equal to the draft: loss and gradient 0 within rounding."""
+    z = (torch.randn(6, 5000, generator=torch.Generator().manual_seed(16)) * 2).cuda()
+    top = osd.osd_topk(z, 50)
+    for kind in ("fkl", "rkl", "jsd", "tvd"):
+        loss, grad = osd.osd_distill_topk(z, top, None, kind)
+        # errors of 5e-6 in log p and log q (see REL), the loss of them to the first order
+        assert loss.abs().max() < 1e-5 and grad.abs().max() < 1e-5 or kind == "tvd"
+        assert loss.abs().max() < 1e-5
+
+
+def test_gradient_against_differences(osd):
+    """The loss of the kernel itself, moved along its gradient: central differences in fp32 of a
+    step h = 0.05 have an error of h^2/6 |l'''| (|l'''| <= 2 along a unit vector at tau = 1) plus 2^-20/h."""
+    z, top = _inputs(8, 512, 20, torch.float32, 17)
+    z, top = z.cuda(), _cuda(top)
+    for kind in ("fkl", "rkl", "jsd", "ce"):
+        loss, grad = osd.osd_distill_topk(z, top, None, kind)
+        d = grad / grad.norm(dim=1, keepdim=True)
+        up, _ = osd.osd_distill_topk(z + 0.05 * d, top, None, kind)
+        dn, _ = osd.osd_distill_topk(z - 0.05 * d, top, None, kind)
+        diff = (up - dn) / 0.1
+        assert torch.all((diff - grad.norm(dim=1)).abs() <= 0.05 ** 2 / 3 + 2e-5)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_views_masks_and_given_outputs(osd, dtype):
+    B, P, V, K = 6, 3, 1501, 30
+    z, top = _inputs(B * P, V, K, dtype, 18)
+    wide = torch.zeros(P + 1, B, V + 4, dtype=dtype, device="cuda")
+    wide[:P, :, 3:V + 3] = z.view(B, P, V).transpose(0, 1).cuda()
+    view = wide[:P, :, 3:V + 3].transpose(0, 1)
+    shaped = (top[0].view(B, P, K).cuda(), top[1].view(B, P, K).cuda(), top[2].view(B, P).cuda())
+    mask = (torch.arange(B * P) % 3 != 1).to(torch.uint8).view(B, P)
+    dl, ls = torch.full((B, P, V), 7.0, device="cuda"), torch.full((B, P), 7.0, device="cuda")
+    on = mask.bool().view(-1)
+    for kind in KINDS:
+        dl.fill_(7.0)
+        a, b = osd.osd_distill_topk(view, shaped, mask.cuda(), kind, loss=ls, dlogits=dl)
+        assert a is ls and b is dl
+        assert (ls.view(-1)[~on] == 0).all() and (dl.view(-1, V)[~on] == 7).all()
+        _compare(ls.view(-1)[on], dl.view(-1, V)[on], z[on], tuple(t[on] for t in top), kind, 0.5, 1.0)
+    # one row of logits against several teachers
+    one = z[:1].cuda().expand(B * P, V)
+    loss, grad = osd.osd_distill_topk(one, _cuda(top), None, "rkl")
+    _compare(loss, grad, z[:1].expand(B * P, V), top, "rkl", 0.5, 1.0)
+    none, nog = osd.osd_distill_topk(z[:0].cuda(), _cuda(tuple(t[:0] for t in top)))
+    assert none.shape == (0,) and nog.shape == (0, V)
+
+
+def test_offsets_past_32_bits(osd):
+    V, far = 2000, (1 << 31) + 8 * 13
+    z, top = _inputs(2, V, 9, torch.bfloat16, 19)
+    view = torch.zeros(far + V, dtype=torch.bfloat16, device="cuda").as_strided((2, V), (far, 1))
+    view.copy_(z.cuda())
+    loss, grad = osd.osd_distill_topk(view, _cuda(top), None, "jsd")
+    _compare(loss, grad, z, top, "jsd", 0.5, 1.0)
+
+
+def test_gradient_rows_past_32_bits(osd):
+    """More than 2^31 gradient entries."""
+    V, N = 32000, 68000
+    z = torch.zeros(N, V, dtype=torch.bfloat16, device="cuda")
+    row, top = _inputs(1, V, 16, torch.bfloat16, 20)
+    z[-1] = row[0].cuda()
+    mask = torch.zeros(N, dtype=torch.uint8, device="cuda")
+    mask[-1] = 1
+    full = (torch.zeros(N, 16, device="cuda"), torch.zeros(N, 16, dtype=torch.int32, device="cuda"), torch.zeros(N, device="cuda"))
+    for f, t in zip(full, top):
+        f[-1] = t[0].cuda()
+    loss, grad = osd.osd_distill_topk(z, full, mask, "rkl")
+    _compare(loss[-1:], grad[-1:], row, top, "rkl", 0.5, 1.0)
+    assert (loss[:-1] == 0).all()
+
+
+def test_one_step_of_all_three(osd):
+    """Verification, the rejected rows kept, and distillation from them, as one captured step that is
+    replayed on new inputs; and the same on a side stream."""
+    B, k, V, K = 24, 4, 8000, 32
+    g = torch.Generator().manual_seed(21)
+
+    def inputs():
+        z = (torch.randn(B, k, V, generator=g) * 2.5).bfloat16()
+        t = torch.cat([z + torch.randn(B, k, V, generator=g), z[:, :1]], 1).bfloat16()
+        q, p = torch.softmax(z.float(), -1), torch.softmax(t.float(), -1)
+        y = torch.multinomial(q.view(-1, V), 1, generator=g).view(B, k).int()
+        return z, t, q, p, y, torch.rand(B, k + 1, generator=g)
+
+    first, second = inputs(), inputs()
+    z, t, q, p, y, u = static = [x.cuda() for x in first]
+    top = osd.TopkResult(torch.zeros(B, k, K, device="cuda"), torch.full((B, k, K), -1, dtype=torch.int32, device="cuda"),
+                         torch.zeros(B, k, device="cuda"))
+    dl = torch.zeros(B, k, V, device="cuda")
+
+    def step(stream=None):
+        res = osd.osd_verify_probs(q, p, y, u, stream=stream)
+        osd.osd_topk(t[:, :k], K, res.mismatch_mask, out=top, stream=stream)
+        loss, _ = osd.osd_distill_topk(z, top, res.mismatch_mask, "rkl", dlogits=dl, stream=stream)
+        return res, loss
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        res, loss = step()
+    for new in (second, first):
+        for s, x in zip(static, new):
+            s.copy_(x)
+        dl.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        zc, tc, qc, pc, yc, uc = new
+        acc, out, mask = compact.verify_probs(qc, pc, yc.numpy(), uc)
+        np.testing.assert_array_equal(res.out_tokens.cpu().numpy(), out)
+        np.testing.assert_array_equal(res.mismatch_mask.cpu().numpy(), mask)
+        on = torch.tensor(mask.reshape(-1).astype(bool))
+        assert 3 < on.sum() <= B
+        rows = tc[:, :k].reshape(-1, V)[on]
+        v, i, r = compact.topk(rows, K)
+        np.testing.assert_array_equal(top.ids.view(-1, K)[on].cpu().numpy(), i)
+        _compare(loss.view(-1)[on], dl.view(-1, V)[on], zc.reshape(-1, V)[on],
+                 (torch.tensor(v), torch.tensor(i), torch.tensor(r)), "rkl", 0.5, 1.0)
+        assert (loss.view(-1)[~on] == 0).all() and (dl.view(-1, V)[~on] == 0).all()
+    want = dl.clone()
+    dl.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    side.synchronize()
+    assert torch.equal(dl, want)  # no sum depends on the order of its parts
+
+
+def test_two_streams_at_once(osd):
+    cases = [_inputs(300, 32000, 64, torch.bfloat16, 30 + s) for s in range(2)]
+    dev = [(z.cuda(), _cuda(top)) for z, top in cases]
+    want = [osd.osd_distill_topk(z, top, None, "jsd") for z, top in dev]
+    streams = [torch.cuda.Stream() for _ in dev]
+    torch.cuda.synchronize()
+    got = [osd.osd_distill_topk(z, top, None, "jsd", stream=s) for (z, top), s in zip(dev, streams)]
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_native_equals_ctypes_and_refusals(osd, monkeypatch):
+    z, top = _inputs(6, 900, 20, torch.bfloat16, 22)
+    z, top = z.cuda(), _cuda(top)
+    a = osd.osd_distill_topk(z, top, None, "jsd", 0.3, temperature=2)
+    real = osd._binding
+    assert real.distill_topk(z, top, None, "jsd", 0.3, 1.0, None, None, None, None) is not None
+
+    class Nothing:
+        def __getattr__(self, name):
+            return lambda *args: None
+    monkeypatch.setattr(osd, "_binding", Nothing())
+    b = osd.osd_distill_topk(z, list(top), None, "jsd", 0.3, temperature=2)
+    for s, t in zip(a, b):
+        assert s.dtype == t.dtype and torch.equal(s, t)
+    monkeypatch.setattr(osd, "_binding", real)
+    with pytest.raises(osd.OsdError):
+        osd.osd_distill_topk(z, top[:2] + (None,), None, "rkl")
+    with pytest.raises(osd.OsdError):
+        osd.osd_distill_topk(z, top, temperature=0.0)
+    with pytest.raises(ValueError, match="top must"):
+        osd.osd_distill_topk(z, (top[0][:, :5], top[1], top[2]))
+    with pytest.raises(ValueError, match="rest"):
+        osd.osd_distill_topk(z, top[:2] + (top[2].double(),))
+    with pytest.raises(ValueError, match="mask"):
+        osd.osd_distill_topk(z, top, torch.ones(6, device="cuda"))
+    with pytest.raises(KeyError):
+        osd.osd_distill_topk(z, top, loss_kind="kl")
+    with pytest.raises(TypeError, match="float32 or bfloat16"):
+        osd.osd_distill_topk(z.half(), top)

@@ -103,3 +103,77 @@ def test_topk_and_its_rest_make_up_the_row():
         total = np.logaddexp(np.log(np.exp(v / tau).sum(1)), r)
         np.testing.assert_allclose(total, np.log(np.exp(x / tau).sum(1)), rtol=1e-13)
         assert (np.diff(v, axis=1) <= 0).all() and np.array_equal(np.sort(x, axis=1)[:, ::-1][:, :20], v)
+
+
+# ------------------------------------------------------------------ distillation from top logits
+KINDS = ["fkl", "rkl", "jsd", "tvd", "ce"]
+
+
+def _case(seed, V=9, K=4, rest=True):
+    rng = np.random.default_rng(seed)
+    z, t = rng.normal(size=V) * 2, rng.normal(size=(1, V)) * 2
+    v, i, r = compact.topk(t, K, 1.0)
+    return z, v[0], i[0], (r[0] if rest else None)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("tau", [0.5, 1.0, 2.0])
+def test_gradient_against_differences(kind, tau):
+    for seed in range(6):
+        z, v, i, r = _case(seed)
+        if seed == 5:
+            i = np.where(np.arange(len(i)) == 1, -1, i)  # an unused entry: its token joins the others
+        loss, grad, _, _ = compact.distill_topk_row(z, v, i, r, kind, 0.3, tau)
+        for j in range(len(z)):
+            h = 1e-5
+            up, dn = z.copy(), z.copy()
+            up[j] += h
+            dn[j] -= h
+            d = (compact.distill_topk_row(up, v, i, r, kind, 0.3, tau)[0] -
+                 compact.distill_topk_row(dn, v, i, r, kind, 0.3, tau)[0]) / (2 * h)
+            assert grad[j] == pytest.approx(d, abs=1e-8)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_all_entries_kept_is_the_full_distillation(kind):
+    rng = np.random.default_rng(3)
+    z, t = rng.normal(size=(8, 11)) * 2, rng.normal(size=(8, 11)) * 2
+    for tau in (0.7, 1.0):
+        v, i, r = compact.topk(t, 11, tau)
+        assert (r == -np.inf).all()
+        loss, grad, _, _ = compact.distill_topk(z, v, i, r, kind, 0.3, tau)
+        ref_l, ref_g = oracle.distill(z, t, None, kind, 0.3, temperature=tau)
+        np.testing.assert_allclose(loss, ref_l, rtol=1e-10, atol=1e-12)
+        np.testing.assert_allclose(grad, ref_g, rtol=1e-9, atol=1e-12)
+
+
+def test_worked_distill_topk():
+    """Masses in quarters: p = (1/2, 1/4 | 1/4), q = (1/4, 1/4 | 1/4 + 1/4)."""
+    z, v, i = np.zeros(4), np.log([2.0, 1.0]), [2, 0]
+    row = lambda kind, rest=np.log(1.0), **kw: compact.distill_topk_row(z, v, i, rest, kind, **kw)
+    ln2 = np.log(2.0)
+    assert row("fkl")[0] == pytest.approx(0.5 * ln2 - 0.25 * ln2)
+    np.testing.assert_allclose(row("fkl")[1], [0, 0.125, -0.25, 0.125], atol=1e-15)
+    assert row("rkl")[0] == pytest.approx(-0.25 * ln2 + 0.5 * ln2)
+    assert row("tvd")[0] == pytest.approx(0.25)
+    assert row("ce")[0] == pytest.approx(2 * ln2)
+    # teacher cut to its kept tokens: p = (2/3, 1/3)
+    assert row("fkl", None)[0] == pytest.approx(2 / 3 * np.log(8 / 3) + 1 / 3 * np.log(4 / 3))
+    assert row("rkl", None)[0] == np.inf
+    # no target mass, a repeated id, an id past the row
+    assert row("jsd", -np.inf, beta=0.0)[0] == 0.0
+    assert compact.distill_topk_row(z, v, [-1, -1], None, "fkl")[0] == 0.0
+    assert np.isnan(compact.distill_topk_row(z, v, [2, 2], 0.0, "fkl")[0])
+    assert np.isnan(compact.distill_topk_row(z, v, [2, 4], 0.0, "fkl")[0])
+
+
+def test_bucketing_never_raises_a_divergence():
+    """Merging the other tokens into one class loses information: f-divergences cannot grow."""
+    rng = np.random.default_rng(4)
+    z, t = rng.normal(size=(40, 30)) * 2, rng.normal(size=(40, 30)) * 2
+    v, i, r = compact.topk(t, 6)
+    for kind in ("fkl", "rkl", "jsd", "tvd"):
+        full = oracle.distill(z, t, None, kind, 0.4)[0]
+        cut = compact.distill_topk(z, v, i, r, kind, 0.4)
+        assert (cut[0] <= full + 1e-12).all() and (cut[0] >= 0).all()
+        np.testing.assert_allclose(cut[1].sum(1), 0, atol=1e-12)  # shift invariance
