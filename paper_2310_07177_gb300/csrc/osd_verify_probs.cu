@@ -2,14 +2,18 @@
 // Appendix A.1 of the paper) against probabilities the caller has made, with
 // drafts of different lengths and drafts without a distribution.
 //
-// The tests u q(y) < p(y) need two entries a position, all fetched at once; the
-// first failure (or the last draft) says which one pair of rows the extra token is
-// drawn from, and only that pair is read.
+// One thread-block cluster per sequence.  The tests u q(y) < p(y) need two entries a
+// position, all fetched at once; the first failure (or the last draft) says which one
+// pair of rows the extra token is drawn from, and only that pair is read, each CTA its
+// span of the vocabulary: weights summed per sub-tile, the span totals exchanged by
+// st.async, and the CTA whose span holds u W searches the one sub-tile that holds it.
 //
 // Every probability counts as an integer multiple of 2^-62, so the weights
 // max(0, p - q) and all their sums are integers: exact, in any order.
+#include <algorithm>
 #include <climits>
 #include <cstdint>
+#include <type_traits>
 
 #include "osd.h"
 #include "osd_device.cuh"
@@ -18,7 +22,12 @@
 namespace osd {
 
 constexpr int kProbThreads = 256;
-constexpr int kProbWarps = kProbThreads / 32;
+constexpr int kProbMaxCluster = 8;
+constexpr int kProbUnroll = 4;                      // 16-byte vectors of a row per lane and sub-tile
+constexpr uint64_t kProbPeerWaitNs = 3000000000ull;  // bound on the wait for the peers' totals
+
+template <typename In, bool kAligned>                 // entries of a sub-tile
+constexpr int prob_sub = kAligned ? kProbUnroll * 32 * Elem<In>::kVec : 512;
 
 struct ProbParams {
     const void* draft;   // nullable
@@ -31,114 +40,411 @@ struct ProbParams {
     int32_t* accepted;
     int32_t* out_tokens;
     uint8_t* mask;
+    int csize;  // CTAs per sequence
+    int span;   // vocabulary entries per CTA, whole vectors
 };
 
-// x in [0, 2) as a multiple of 2^-62, rounded to nearest, ties to even (0 for others).
-__device__ __forceinline__ unsigned long long fix62(float x) {
-    const uint32_t bits = __float_as_uint(x);
-    const int e = static_cast<int>(bits >> 23);  // with the sign: negative values have e >= 256
-    if (e == 0 || e > 127) return 0ull;          // below 2^-126, or 2 and above
-    const unsigned long long m = (bits & 0x7fffffu) | 0x800000u;
-    const int sh = e - 150 + 62;                 // x = m 2^(e - 150)
-    if (sh >= 0) return m << sh;
-    if (sh < -25) return 0ull;
-    const unsigned long long half = 1ull << (-sh - 1), v = m >> -sh, rem = m & ((half << 1) - 1);
-    return v + ((rem > half || (rem == half && (v & 1ull))) ? 1ull : 0ull);
-}
+// Sums of weights P - Q in units of 2^-62, where P and Q are p and q rounded to that
+// grid.  A value x in [0, 2) goes into three parts, each the mantissa of a sum with a
+// constant whose binade has the wanted step: the nearest multiple of 2^-22 (x + 2), of
+// 2^-44 of what is left of it (exact, as every remainder of such a sum is), of 2^-62 of
+// that.  The mantissas are added as integers; 13 instructions an entry with q, packed in
+// pairs, against about 30 with 64-bit shifts.  Half-way cases round to even as a direct
+// rounding to 2^-62 does, since the first two remainders are exact.
+struct FixSum {
+    int hi = 0, mid = 0, lo = 0;
 
-template <typename In>
-__global__ void __launch_bounds__(kProbThreads) verify_probs_kernel(ProbParams p) {
+    // p, q in pairs; q is taken as min(q, p), so that P - Q is the weight
+    template <bool kQ>
+    __device__ __forceinline__ void add(float2 p, float2 q) {
+        const float2 c1 = f2(2.f), n1 = f2(-2.f), c2 = f2(0x1.8p-21f), n2 = f2(-0x1.8p-21f), c3 = f2(0x1.8p-39f);
+        auto part = [](float2 x, const float2& c) { return add2(x, c); };
+        auto bits = [](float x) { return __float_as_int(x); };
+        const float2 p1 = part(p, c1), rp = sub2(p, add2(p1, n1));
+        const float2 p2 = part(rp, c2), sp = sub2(rp, add2(p2, n2));
+        const float2 p3 = part(sp, c3);
+        if constexpr (kQ) {
+            q = make_float2(fminf(q.x, p.x), fminf(q.y, p.y));
+            const float2 q1 = part(q, c1), rq = sub2(q, add2(q1, n1));
+            const float2 q2 = part(rq, c2), sq = sub2(rq, add2(q2, n2));
+            const float2 q3 = part(sq, c3);
+            hi += (bits(p1.x) - bits(q1.x)) + (bits(p1.y) - bits(q1.y));
+            mid += (bits(p2.x) - bits(q2.x)) + (bits(p2.y) - bits(q2.y));
+            lo += (bits(p3.x) - bits(q3.x)) + (bits(p3.y) - bits(q3.y));
+        } else {
+            hi += (bits(p1.x) - 0x40000000) + (bits(p1.y) - 0x40000000);
+            mid += (bits(p2.x) - 0x35400000) + (bits(p2.y) - 0x35400000);
+            lo += (bits(p3.x) - 0x2c400000) + (bits(p3.y) - 0x2c400000);
+        }
+    }
+    __device__ __forceinline__ unsigned long long total() const {
+        return (static_cast<unsigned long long>(static_cast<long long>(hi)) << 40) +
+               (static_cast<unsigned long long>(static_cast<long long>(mid)) << 18) +
+               static_cast<unsigned long long>(static_cast<long long>(lo));
+    }
+    // the warp's total, in every lane: up to 32 entries a lane keep every part within 32 bits, the middle one,
+    // at most 2^27 a lane, in two halves
+    __device__ __forceinline__ unsigned long long warp_total() const {
+        FixSum s;
+        s.hi = __reduce_add_sync(0xffffffffu, hi);
+        s.lo = __reduce_add_sync(0xffffffffu, lo);
+        s.mid = __reduce_add_sync(0xffffffffu, mid >> 16);
+        const int low = __reduce_add_sync(0xffffffffu, mid & 0xffff);
+        return s.total() - (static_cast<unsigned long long>(static_cast<long long>(s.mid)) << 18) +
+               (static_cast<unsigned long long>(static_cast<long long>(s.mid)) << 34) +
+               (static_cast<unsigned long long>(static_cast<unsigned>(low)) << 18);
+    }
+};
+
+template <typename In> struct Tile {
+    uint4 p[kProbUnroll], q[kProbUnroll];
+};
+
+// Shared memory of a sequence's draw.
+struct ProbSmem {
+    int a, n, y;
+    unsigned long long total, totals[kProbMaxCluster];  // this CTA's, and slot r from CTA r
+    uint64_t bar;
+    unsigned long long W, tau, base;
+    int owner, mode, tile;
+    MaxIdx best[kProbThreads / 32];
+};
+
+template <typename In, bool kAligned>
+__global__ void __launch_bounds__(kProbThreads, 4) verify_probs_kernel(ProbParams p) {
     using E = Elem<In>;
-    __shared__ unsigned long long s_warp[kProbWarps];
-    __shared__ int s_a, s_n, s_y;
+    constexpr int kW = E::kVec, kT = kProbThreads, kWarps = kT / 32, kSub = prob_sub<In, kAligned>;
+    constexpr int kSingle = kSub / 32;  // off the 16-byte grid: entries a lane and sub-tile
+    __shared__ ProbSmem sh;
+    extern __shared__ unsigned long long s_sub[];  // a total per sub-tile of the span
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int b = blockIdx.x, k = p.k, V = p.V;
+    const int csize = p.csize, rank = csize > 1 ? static_cast<int>(cluster_rank()) : 0;
+    const int b = blockIdx.x / csize, k = p.k, V = p.V;
+    if (tid == 0) {
+        mbar_init_only(&sh.bar, 1);
+        fence_mbarrier_init();
+    }
     grid_dependency_sync();
+    if (csize > 1) cluster_arrive_relaxed();  // peers may push once this CTA's barrier is there
     const In* target = static_cast<const In*>(p.target) + b * p.tsb;
     const In* draft = p.draft ? static_cast<const In*>(p.draft) + b * p.dsb : nullptr;
     const int32_t* y = p.tokens + size_t(b) * k;
     const float* u = p.uniforms + size_t(b) * (k + 1);
     int32_t* out = p.out_tokens + size_t(b) * (k + 1);
+    // ---- the tests, by every CTA alike: all positions' entries at once, the first failure counts
     if (warp == 0) {
         const int n = p.lens ? p.lens[b] : k;
+        constexpr int kC = OSD_VERIFY_MAX_K / 32;
+        int t[kC];
+        float uu[kC];
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {  // (in flight with the length)
+            const int i = c * 32 + lane;
+            t[c] = i < k ? y[i] : 0;
+            uu[c] = i < k ? u[i] : 0.f;
+        }
         bool bad = n < 0 || n > k;
         int a = n;
-        for (int c = 0; c < n && !bad; c += 32) {
-            const int i = c + lane;
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+            const int i = c * 32 + lane;
             bool fail = false, off = false;
-            if (i < n) {
-                const int t = y[i];
-                off = t < 0 || t >= V;
+            if (!bad && i < n) {
+                off = t[c] < 0 || t[c] >= V;
                 if (!off) {
-                    const float py = E::load(target + i * p.tsi + t), qy = draft ? E::load(draft + i * p.dsi + t) : 1.f;
-                    fail = !(static_cast<double>(u[i]) * static_cast<double>(qy) < static_cast<double>(py));  // exact
+                    const float py = E::load(target + i * p.tsi + t[c]), qy = draft ? E::load(draft + i * p.dsi + t[c]) : 1.f;
+                    fail = !(static_cast<double>(uu[c]) * static_cast<double>(qy) < static_cast<double>(py));  // exact
                 }
             }
-            bad = __any_sync(0xffffffffu, off);
+            bad = bad || __any_sync(0xffffffffu, off);
             const unsigned f = __ballot_sync(0xffffffffu, fail);
-            if (f && a == n) a = c + __ffs(f) - 1;
+            if (f && a == n) a = c * 32 + __ffs(f) - 1;
+        }
+        int ya = 0;
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+            const int v = __shfl_sync(0xffffffffu, t[c], a & 31);
+            if (a >> 5 == c) ya = v;
         }
         if (lane == 0) {
-            s_a = bad ? -1 : a;
-            s_n = n;
-            s_y = (!bad && a < n) ? y[a] : -1;
+            sh.a = bad ? -1 : a;
+            sh.n = n;
+            sh.y = ya;
+        }
+        if (rank == 0) {
+#pragma unroll
+            for (int c = 0; c < kC; ++c) {
+                const int i = c * 32 + lane;
+                if (i < k) {
+                    if (bad || i != a) out[i] = !bad && i < a ? t[c] : -1;
+                    p.mask[size_t(b) * k + i] = (!bad && i == a && a < n) ? 1 : 0;
+                }
+            }
+            if (lane == 0) {
+                p.accepted[b] = bad ? -1 : a;
+                if (bad || a < k) out[k] = -1;
+            }
         }
     }
     __syncthreads();
-    const int a = s_a, n = s_n;
-    if (tid == 0) p.accepted[b] = a;
-    for (int i = tid; i <= k; i += kProbThreads)
-        if (i != a) out[i] = i < a ? y[i] : -1;
-    for (int i = tid; i < k; i += kProbThreads) p.mask[size_t(b) * k + i] = (i == a && a < n) ? 1 : 0;
-    if (a < 0) return;
+    const int a = sh.a;
+    if (csize > 1) cluster_wait();
+    if (a < 0) return;  // the whole cluster alike, before any push
+    const bool reject = a < sh.n;
     const In* prow = target + a * p.tsi;
-    const In* qrow = (draft && a < n) ? draft + a * p.dsi : nullptr;
-    const int hot = draft ? -1 : s_y;  // the entry a draft without a distribution holds
-    auto weight = [&](int j) -> unsigned long long {
-        const unsigned long long P = fix62(E::load(prow + j));
-        const unsigned long long Q = qrow ? fix62(E::load(qrow + j)) : (j == hot ? 1ull << 62 : 0ull);
-        return P > Q ? P - Q : 0ull;
+    const In* qrow = (draft && reject) ? draft + a * p.dsi : nullptr;
+    const int hot = (!draft && reject) ? sh.y : -1;  // the entry a draft without a distribution holds
+    const int e0 = rank * p.span, e1 = min(V, e0 + p.span);
+    const int nsub = (e1 - e0 + kSub - 1) / kSub;
+
+    // ---- the span's weights, a total per sub-tile.  On the 16-byte grid a lane takes vectors
+    // of a sub-tile; off it single entries, 32 neighbours a load (shifting vectors into place cost more
+    // than the wider loads saved: 600 x 4 x 32001 fp32 44.2 us, against 31.8, bf16 40.1 and 27.4)
+    Tile<In> t;  // the last sub-tile of this warp stays here for the search
+    auto vector_at = [&](int s, int i) { return e0 + s * kSub + (i * 32 + lane) * kW; };
+    auto load = [&](auto has_q, int s) {
+        constexpr bool kQ = decltype(has_q)::value;
+        auto row = [&](const In* r, uint4* v) {
+#pragma unroll
+            for (int i = 0; i < kProbUnroll; ++i) {
+                const int j = vector_at(s, i);
+                if (j + kW <= e1) {
+                    v[i] = ldg_stream(r + j);
+                } else {
+                    float x[kW];
+#pragma unroll
+                    for (int e = 0; e < kW; ++e) x[e] = j + e < e1 ? E::load(r + j + e) : 0.f;
+                    v[i] = pack_raw<In, kW>(x);
+                }
+            }
+        };
+        row(prow, t.p);
+        if constexpr (kQ) row(qrow, t.q);
     };
-    const int per = (V + kProbWarps - 1) / kProbWarps;
-    const int j0 = min(V, warp * per), j1 = min(V, j0 + per);
-    unsigned long long mine = 0ull;
-    for (int j = j0 + lane; j < j1; j += 32) mine += weight(j);
-    mine = warp_sum_u64(mine);
-    if (lane == 0) s_warp[warp] = mine;
-    __syncthreads();
-    unsigned long long W = 0ull, base = 0ull;
-    for (int w = 0; w < kProbWarps; ++w) W += s_warp[w];
-    const unsigned long long tau = fix_scale(u[k], W);
-    int owner = -1;
-    if (W > 0ull && tau < W) {
-        // (bounded: the sums of rows outside the domain may wrap)
-        for (owner = 0; owner < kProbWarps - 1 && base + s_warp[owner] <= tau; ++owner) base += s_warp[owner];
-    }
-    if (owner >= 0 ? warp == owner : warp == 0) {
-        int token = -1;
-        if (owner >= 0) {
-            for (int c = j0; c < j1 && token < 0; c += 32) {
-                const unsigned long long w = c + lane < j1 ? weight(c + lane) : 0ull;
-                const unsigned long long incl = base + warp_incl_scan_u64(w);
-                const unsigned hit = __ballot_sync(0xffffffffu, incl > tau);
-                if (hit) token = c + __ffs(hit) - 1;
-                base = __shfl_sync(0xffffffffu, incl, 31);
-            }
-        } else if (W > 0ull) {  // u >= 1: the largest entry with weight
-            for (int j = lane; j < V; j += 32)
-                if (weight(j)) token = j;
-            token = warp_reduce(token, [](int x, int z) { return max(x, z); });
-        } else {  // no weight anywhere: the first maximum of p_a
-            MaxIdx acc{kNegInf, INT_MAX};
-            for (int j = lane; j < V; j += 32) {
-                const float x = E::load(prow + j);
-                if (x > acc.m) acc = MaxIdx{x, j};
-            }
-            acc = warp_reduce(acc, [](MaxIdx x, MaxIdx z) { return merge_mi(x, z); });
-            token = acc.i;
+    // entries [j, j + kN) of both rows into the sums
+    auto sum = [&](auto has_q, float* x, const float* z, int j, auto count, FixSum& acc) {
+        constexpr bool kQ = decltype(has_q)::value;
+        constexpr int kN = decltype(count)::value;
+        if (!kQ && static_cast<unsigned>(hot - j) < static_cast<unsigned>(kN)) {
+#pragma unroll
+            for (int e = 0; e < kN; ++e)
+                if (j + e == hot) x[e] = fmaxf(x[e] - 1.f, 0.f);  // exact
         }
-        if (lane == 0) out[a] = (token >= 0 && token < V) ? token : 0;
+#pragma unroll
+        for (int e = 0; e < kN; e += 2)
+            acc.template add<kQ>(make_float2(x[e], x[e + 1]), kQ ? make_float2(z[e], z[e + 1]) : make_float2(0.f, 0.f));
+    };
+    auto vector_sum = [&](auto has_q, int s, int i, FixSum& acc) {
+        float x[kW], z[kW];
+        E::unpack(t.p[i], x);
+        if constexpr (decltype(has_q)::value) E::unpack(t.q[i], z);
+        sum(has_q, x, z, vector_at(s, i), std::integral_constant<int, kW>(), acc);
+    };
+    auto sums = [&](auto has_q) {
+        constexpr bool kQ = decltype(has_q)::value;
+        for (int s = warp; s < nsub; s += kWarps) {
+            FixSum acc;
+            if constexpr (kAligned) {
+                load(has_q, s);
+#pragma unroll
+                for (int i = 0; i < kProbUnroll; ++i) vector_sum(has_q, s, i, acc);
+            } else {
+                float x[kSingle], z[kSingle];
+                const int j0 = e0 + s * kSub + lane;
+#pragma unroll
+                for (int e = 0; e < kSingle; ++e) x[e] = j0 + e * 32 < e1 ? E::load(prow + j0 + e * 32) : 0.f;
+                if constexpr (kQ) {
+#pragma unroll
+                    for (int e = 0; e < kSingle; ++e) z[e] = j0 + e * 32 < e1 ? E::load(qrow + j0 + e * 32) : 0.f;
+                }
+                if (!kQ && static_cast<unsigned>(hot - (j0 - lane)) < static_cast<unsigned>(kSub)) {
+#pragma unroll
+                    for (int e = 0; e < kSingle; ++e)
+                        if (j0 + e * 32 == hot) x[e] = fmaxf(x[e] - 1.f, 0.f);
+                }
+#pragma unroll
+                for (int e = 0; e < kSingle; e += 2)
+                    acc.template add<kQ>(make_float2(x[e], x[e + 1]), kQ ? make_float2(z[e], z[e + 1]) : make_float2(0.f, 0.f));
+            }
+            const unsigned long long w = acc.warp_total();
+            if (lane == 0) s_sub[s] = w;
+        }
+    };
+    if (qrow) sums(std::true_type());
+    else sums(std::false_type());
+    __syncthreads();
+    // ---- the cluster's totals, W, u W and whose span holds it, by warp 0 of every CTA alike
+    if (warp == 0) {
+        unsigned long long mine = 0ull;
+        for (int s = lane; s < nsub; s += 32) mine += s_sub[s];
+        mine = warp_sum_u64(mine);
+        bool got = true;
+        if (csize > 1) {
+            if (lane < csize)
+                st_async_u64(map_rank(&sh.totals[rank], static_cast<uint32_t>(lane)), mine,
+                             map_rank(&sh.bar, static_cast<uint32_t>(lane)));
+            if (lane == 0) mbar_arrive_expect_tx(&sh.bar, static_cast<uint32_t>(csize) * 8u);
+            got = __all_sync(0xffffffffu, mbar_wait_cluster_bounded(&sh.bar, 0, kProbPeerWaitNs));
+        }
+        const unsigned long long tot = lane < csize ? (csize > 1 ? sh.totals[lane] : mine) : 0ull;
+        const unsigned long long incl = warp_incl_scan_u64(tot);
+        const unsigned long long W = __shfl_sync(0xffffffffu, incl, 31), tau = fix_scale(u[k], W);
+        // 0: the entry that holds u W; 1: the last entry with weight (u >= 1); 2: no weight at all
+        int mode = W == 0ull ? 2 : (tau < W ? 0 : 1), owner = 0, tile = 0;
+        unsigned long long base = 0ull;
+        if (mode == 0) {
+            owner = min(__ffs(__ballot_sync(0xffffffffu, incl > tau)) - 1, csize - 1);
+            base = __shfl_sync(0xffffffffu, incl - tot, max(owner, 0));
+        } else if (mode == 1) {
+            owner = 31 - __clz(__ballot_sync(0xffffffffu, tot > 0ull));
+        }
+        if (rank == owner && mode != 2) {
+            // the sub-tile: each lane owns a run of consecutive ones
+            const int per = (nsub + 31) / 32;
+            const int lo = min(nsub, lane * per), hi = min(nsub, lo + per);
+            unsigned long long run = 0ull;
+            for (int s = lo; s < hi; ++s) run += s_sub[s];
+            unsigned long long before = base + warp_incl_scan_u64(run) - run;
+            int found = -1;
+            if (mode == 0) {
+                for (int s = lo; s < hi && found < 0; ++s) {
+                    if (before + s_sub[s] > tau && before <= tau) found = s;
+                    else before += s_sub[s];
+                }
+                const unsigned hit = __ballot_sync(0xffffffffu, found >= 0);
+                const int l = hit ? __ffs(hit) - 1 : 0;
+                found = __shfl_sync(0xffffffffu, found, l);
+                base = __shfl_sync(0xffffffffu, before, l);
+            } else {
+                for (int s = lo; s < hi; ++s)
+                    if (s_sub[s]) found = s;
+                for (int o = 16; o > 0; o >>= 1) found = max(found, __shfl_xor_sync(0xffffffffu, found, o));
+            }
+            tile = max(found, 0);
+        }
+        if (lane == 0) {
+            sh.owner = got ? owner : -1;
+            sh.mode = mode;
+            sh.tau = tau;
+            sh.base = base;
+            sh.tile = tile;
+        }
     }
+    __syncthreads();
+    if (sh.owner < 0) {  // a peer's total did not arrive in time: the sequence is reported as bad
+        if (tid == 0) p.accepted[b] = -1;
+        for (int i = tid; i <= k; i += kT) out[i] = -1;
+        for (int i = tid; i < k; i += kT) p.mask[size_t(b) * k + i] = 0;
+        return;
+    }
+    if (rank != sh.owner) return;
+    if (sh.mode == 2) {  // the first maximum of p_a
+        MaxIdx best{kNegInf, INT_MAX};
+#pragma unroll 8
+        for (int j = tid; j < V; j += kT) {
+            const float x = E::load(prow + j);
+            if (x > best.m) best = MaxIdx{x, j};
+        }
+        best = block_reduce<kT>(best, [](MaxIdx x, MaxIdx z) { return merge_mi(x, z); }, sh.best);
+        if (tid == 0) out[a] = best.i < V ? best.i : 0;
+        return;
+    }
+    // ---- the entry, by the warp that summed the one sub-tile: totals of a few entries a lane,
+    // scanned in order
+    if (warp == sh.tile % kWarps) {
+        const unsigned long long tau = sh.tau;
+        const int s = sh.tile, mode = sh.mode;
+        unsigned long long base = sh.base;
+        int token = -1;
+        // this lane's kN entries from j on; those of lower lanes come before them
+        auto step = [&](auto has_q, float* x, const float* z, int j, auto count) {
+            constexpr bool kQ = decltype(has_q)::value;
+            constexpr int kN = decltype(count)::value;
+            FixSum acc;
+            sum(has_q, x, z, j, count, acc);  // (takes 1 from the entry `hot`)
+            const unsigned long long mine = acc.total(), incl = base + warp_incl_scan_u64(mine);
+            const bool here = mode == 0 ? (token < 0 && incl > tau && incl - mine <= tau) : mine > 0ull;
+            const unsigned hit = __ballot_sync(0xffffffffu, here);
+            if (hit) {
+                const int l = mode == 0 ? __ffs(hit) - 1 : 31 - __clz(hit);
+                int at = -1;
+                if (lane == l) {
+                    unsigned long long c = incl - mine;
+#pragma unroll
+                    for (int e = 0; e < kN; ++e) {
+                        FixSum one;
+                        one.template add<kQ>(make_float2(x[e], 0.f), make_float2(kQ ? z[e] : 0.f, 0.f));
+                        const unsigned long long w = one.total();
+                        c += w;
+                        if (mode == 0 ? (at < 0 && c > tau) : w > 0ull) at = j + e;
+                    }
+                }
+                token = __shfl_sync(0xffffffffu, at, l);
+            }
+            base = __shfl_sync(0xffffffffu, incl, 31);
+        };
+        auto search = [&](auto has_q) {
+            [[maybe_unused]] constexpr bool kQ = decltype(has_q)::value;
+            if constexpr (kAligned) {
+                if (s + kWarps < nsub) load(has_q, s);
+#pragma unroll
+                for (int i = 0; i < kProbUnroll; ++i) {
+                    float x[kW], z[kW];
+                    E::unpack(t.p[i], x);
+                    if constexpr (kQ) E::unpack(t.q[i], z);
+                    step(has_q, x, z, vector_at(s, i), std::integral_constant<int, kW>());
+                }
+            } else {
+                float x[kSingle], z[kSingle];
+                const int j = e0 + s * kSub + lane * kSingle;
+#pragma unroll
+                for (int e = 0; e < kSingle; ++e) {
+                    x[e] = j + e < e1 ? E::load(prow + j + e) : 0.f;
+                    z[e] = kQ && j + e < e1 ? E::load(qrow + j + e) : 0.f;
+                }
+                step(has_q, x, z, j, std::integral_constant<int, kSingle>());
+            }
+            // (rows outside the domain, whose sums wrap, may hold no such entry)
+            if (lane == 0) out[a] = token >= 0 && token < V ? token : 0;
+        };
+        if (qrow) search(std::true_type());
+        else search(std::false_type());
+    }
+}
+
+// Split V over at most c CTAs in spans of whole 128-byte lines.
+static void split_probs(int V, int c, ProbParams* pp) {
+    const int s = (V + c - 1) / c;
+    pp->span = (s + 63) / 64 * 64;
+    pp->csize = (V + pp->span - 1) / pp->span;
+}
+
+// One wave of the widest clusters that it holds: 256 x 8 x 128256 fp32 44.7 us with 2 CTAs a
+// sequence (512 of 608 slots), 47.5 and 49.7 with 4 and 1; 64 x 4 x 32000 fp32 8.4 with 8, 9.1 and 10.6 with 4
+// and 2.  Batches past one wave take a CTA a sequence (600 x 4 x 32000 27.3, 30.5 with 2), but 2 where that
+// would leave a third of the slots empty and rows are long (400 x 4 x 128256 bf16 48.5, 56.8 with 1; at 128 KB a
+// row 24.4 and 22.1).
+template <typename In, bool kAligned>
+static osd_status launch_probs(ProbParams pp, int B, cudaStream_t s) {
+    constexpr int kSub = prob_sub<In, kAligned>;
+    constexpr size_t kMostSums = 4096;  // of a span of any V over 8 CTAs: what the question below is asked with
+    const long long row = (long long)pp.V * (long long)sizeof(In);
+    const int most = std::max(1, std::min<int>(kProbMaxCluster, int(row / 2048)));  // spans of 2 KB or more
+    int c = std::max(1, widest_cluster<verify_probs_kernel<In, kAligned>, kProbThreads>(B, most, kMostSums, true));
+    if (c == 1 && most > 1 && row >= 192 * 1024 && B <= device_sms() * 8 / 3) c = 2;
+    split_probs(pp.V, c, &pp);
+    const size_t smem = size_t((pp.span + kSub - 1) / kSub) * sizeof(unsigned long long);
+    if ((long long)B * pp.csize > INT_MAX) return OSD_ERR_UNSUPPORTED;
+    return from_cuda(launch_ex(true, verify_probs_kernel<In, kAligned>, dim3(unsigned(B) * unsigned(pp.csize)),
+                               dim3(kProbThreads), smem, s, pp.csize, pp));
+}
+
+template <typename In>
+static osd_status launch_probs_dtype(ProbParams pp, int B, cudaStream_t s) {
+    auto row_ok = [](long long stride, int n) { return n <= 1 || (stride * (long long)sizeof(In)) % 16 == 0; };
+    const bool aligned = aligned_to(pp.target, 16) && row_ok(pp.tsb, B) && row_ok(pp.tsi, pp.k + 1) &&
+                         (!pp.draft || (aligned_to(pp.draft, 16) && row_ok(pp.dsb, B) && row_ok(pp.dsi, pp.k)));
+    return aligned ? launch_probs<In, true>(pp, B, s) : launch_probs<In, false>(pp, B, s);
 }
 
 }  // namespace osd
@@ -161,9 +467,7 @@ extern "C" osd_status osd_verify_probs(const void* draft_probs, const void* targ
         !aligned_to(draft_lens, 4) || !aligned_to(uniforms, 4) || !aligned_to(accepted, 4) || !aligned_to(out_tokens, 4))
         return OSD_ERR_INVALID_ARG;
     ProbParams pp = {draft_probs, target_probs, k, V, d_stride_b, d_stride_i, t_stride_b, t_stride_i,
-                     draft_tokens, draft_lens, uniforms, accepted, out_tokens, mismatch_mask};
+                     draft_tokens, draft_lens, uniforms, accepted, out_tokens, mismatch_mask, 1, V};
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const dim3 grid(static_cast<unsigned>(B)), block(kProbThreads);
-    return from_cuda(dtype == OSD_BF16 ? launch_ex(true, verify_probs_kernel<__nv_bfloat16>, grid, block, 0, s, 1, pp)
-                                       : launch_ex(true, verify_probs_kernel<float>, grid, block, 0, s, 1, pp));
+    return dtype == OSD_BF16 ? launch_probs_dtype<__nv_bfloat16>(pp, B, s) : launch_probs_dtype<float>(pp, B, s);
 }
