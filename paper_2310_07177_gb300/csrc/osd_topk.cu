@@ -35,9 +35,10 @@ namespace osd {
 
 constexpr int kTopThreads = 256;
 constexpr int kTopMaxCluster = 8;
-constexpr int kTopCountMost = 384;   // candidates ranked by counting; more are sorted
-// Exponentials at most 1 of entries whose order is that of atomics are added as whole multiples of
-// 2^-40, so that the sums do not depend on it.
+constexpr int kTopBins = 512;        // bins of a histogram over a range of keys
+constexpr int kTopCrowd = 48;        // candidates of one bin that are ranked by comparing; with more all are sorted
+// Exponentials (at most 1) of candidates, whose order is that of atomics, are added as whole multiples
+// of 2^-40, so that the sum does not depend on it.
 constexpr float kTopFix = 0x1p40f;
 constexpr uint64_t kTopWaitNs = 1000000000ull;  // bound on the wait for the bulk copies
 
@@ -82,13 +83,14 @@ struct TopSmem {
     TopPart parts[2][kTopMaxCluster];  // slot r from CTA r; alternately
     TopPart mine;
     uint64_t bar;
-    int counts[33];
-    int n, hits, err, total;
-    uint32_t kmax, kmin;
+    int n, err, crowd;
+    int bin, reach, above;  // of a histogram: the bin of the K-th largest, entries from it on, past it
     float ref;
+    unsigned long long left;
     int warp_i[kTopThreads / 32];
     float warp_f[kTopThreads / 32];
-    unsigned long long warp_u[kTopThreads / 32];
+    uint32_t warp_hi[kTopThreads / 32], warp_lo[kTopThreads / 32];
+    __align__(16) int hist[kTopBins], base[kTopBins];  // entries per bin, and in the bins above it
 };
 
 __device__ __forceinline__ void st_dsmem_v4(uint32_t addr, int a, int b, float c, float d) {
@@ -126,17 +128,18 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
     const int p0 = rank * p.span, p1 = min(p0 + p.span, V + ph);  // this CTA's positions
     In* staged = reinterpret_cast<In*>(dsm);
     unsigned long long* cand = reinterpret_cast<unsigned long long*>(dsm + size_t(p.section) * sizeof(In));
-    uint32_t* list = reinterpret_cast<uint32_t*>(cand + p.room);
-    uint32_t* maxima = list + p.room;
+    unsigned long long* sorted = cand + p.room;
+    // chunks with an entry from theta on, a part for every warp
+    const int list_room = p.room / 4;
+    unsigned short* list = reinterpret_cast<unsigned short*>(sorted + p.room) + warp * list_room;
+    uint32_t* maxima = reinterpret_cast<uint32_t*>(sorted + p.room) + p.room;
     const int sections = max(1, (p1 - p0 + p.section - 1) / p.section);  // (a CTA past the row's end has an empty one)
     unsigned parity = 0;
     if (tid == 0) {
         sh.err = 0;
         sh.n = 0;
-        sh.kmax = 0u;
-        sh.kmin = 0xffffffffu;
+        sh.left = 0ull;
     }
-    if (tid < 33) sh.counts[tid] = 0;
     __syncthreads();
 
     // Positions [s0, s0 + section) of this CTA into shared memory; what lies outside the row reads as -inf.
@@ -216,13 +219,18 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
     sweep([&](int n, int) {
         for (int k = 0; k < g; ++k) {
             float m = kNegInf;
-            bool any = false;
-            for (int v = tid + k * kT; v < n; v += kT * g) {
-                m = fmaxf(m, E::max_raw(lds_v4(staged + v * kW)));
-                any = true;
+            const int first = tid + k * kT, step = kT * g;
+            int v = first;
+            for (; v + 3 * step < n; v += 4 * step) {  // (four loads in flight)
+                uint4 r[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r[i] = lds_v4(staged + (v + i * step) * kW);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) m = fmaxf(m, E::max_raw(r[i]));
             }
-            if (any) {
-                uint32_t& at = maxima[mine_at + k * kT + tid];
+            for (; v < n; v += step) m = fmaxf(m, E::max_raw(lds_v4(staged + v * kW)));
+            if (first < n) {
+                uint32_t& at = maxima[mine_at + first];
                 at = max(at, key_of(m));
             }
         }
@@ -238,62 +246,121 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
         cluster_wait();
     }
     const int total = kT * g * csize;
+    uint32_t kmax, kmin;  // the largest, and the smallest of a group that has entries
     {
         uint32_t hi = 0u, lo = 0xffffffffu;
         for (int i = tid; i < total; i += kT) {
-            hi = max(hi, maxima[i]);
-            lo = min(lo, maxima[i]);
+            const uint32_t k = maxima[i];
+            hi = max(hi, k);
+            if (k) lo = min(lo, k);
         }
         hi = __reduce_max_sync(0xffffffffu, hi);
         lo = __reduce_min_sync(0xffffffffu, lo);
         if (lane == 0) {
-            atomicMax(&sh.kmax, hi);
-            atomicMin(&sh.kmin, lo);
+            sh.warp_hi[warp] = hi;
+            sh.warp_lo[warp] = lo;
         }
+        for (int i = tid; i < kTopBins; i += kT) sh.hist[i] = 0;
         __syncthreads();
+        kmax = sh.warp_hi[0];
+        kmin = sh.warp_lo[0];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) {
+            kmax = max(kmax, sh.warp_hi[w]);
+            kmin = min(kmin, sh.warp_lo[w]);
+        }
     }
-    // the largest T that K maxima reach, from the highest bit in which they differ on, until few more reach it
-    uint32_t T;
-    {
-        const uint32_t diff = sh.kmax ^ sh.kmin;
-        const int top = diff ? 31 - __clz(diff) : -1;
-        T = top >= 0 ? sh.kmin & ~((2u << top) - 1u) : sh.kmin;
-        if (total < K) T = 0u;
-        constexpr int kLast = sizeof(In) == 2 ? 16 : 0;
-        for (int bit = top; bit >= kLast && total >= K; --bit) {
-            const uint32_t at = T | (1u << bit);
-            int n = 0;
-            for (int i = tid; i < total; i += kT) n += maxima[i] >= at ? 1 : 0;
-            n = __reduce_add_sync(0xffffffffu, n);
-            if (lane == 0 && n) atomicAdd(&sh.counts[bit], n);
-            __syncthreads();
-            n = sh.counts[bit];
-            if (n >= K) {
-                T = at;
-                if (n <= K + K / 8 + 4) break;
+    auto shift_of = [](uint32_t range) { return max(0, 32 - __clz(range) - 9); };  // range >> it < 512 bins
+    // warp 0: from the histogram, the entries in the bins above each (base), the highest bin from which on there are
+    // `need`, and the fullest bin
+    auto scan_bins = [&](int need) {
+        constexpr int kPer = kTopBins / 32;
+        int h[kPer], sum = 0, most = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; i += 4) {
+            const int4 v = *reinterpret_cast<const int4*>(&sh.hist[lane * kPer + i]);
+            h[i] = v.x; h[i + 1] = v.y; h[i + 2] = v.z; h[i + 3] = v.w;
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            sum += h[i];
+            most = max(most, h[i]);
+        }
+        int incl = sum;  // of this lane's bins and all above
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_down_sync(0xffffffffu, incl, o);
+            if (lane + o < 32) incl += y;
+        }
+        int above = incl - sum, bin = -1, reach = 0, past = 0;
+#pragma unroll
+        for (int i = kPer - 1; i >= 0; --i) {
+            sh.base[lane * kPer + i] = above;
+            if (above < need && above + h[i] >= need) {
+                bin = lane * kPer + i;
+                reach = above + h[i];
+                past = above;
             }
+            above += h[i];
+        }
+        most = __reduce_max_sync(0xffffffffu, most);
+        const unsigned has = __ballot_sync(0xffffffffu, bin >= 0);
+        if (lane == (has ? __ffs(has) - 1 : 0)) {
+            sh.bin = bin;
+            sh.reach = reach;
+            sh.above = past;
+            sh.crowd = most;
+        }
+    };
+    // T: reached by K maxima or more, and by few more, from a histogram over the range of the maxima, refined in
+    // the bin of the K-th largest where that holds many (a row with a few entries far above the others)
+    uint32_t T = 0u;
+    {
+        uint32_t lo = kmin, hi = kmax;
+        int above = 0;
+        while (lo <= hi) {
+            const int shift = shift_of(hi - lo);
+            for (int i = tid; i < total; i += kT) {
+                const uint32_t k = maxima[i];
+                if (k >= lo && k <= hi) atomicAdd(&sh.hist[(k - lo) >> shift], 1);
+            }
+            __syncthreads();
+            if (warp == 0) scan_bins(K - above);
+            __syncthreads();
+            const int bin = sh.bin;
+            if (bin < 0) break;  // fewer than K groups
+            T = lo + (static_cast<uint32_t>(bin) << shift);
+            if (above + sh.reach <= K + K / 8 + 4 || shift == 0) break;
+            above += sh.above;
+            lo = T;
+            hi = min(hi, T + ((1u << shift) - 1u));
+            for (int i = tid; i < kTopBins; i += kT) sh.hist[i] = 0;
+            __syncthreads();
         }
         T = max(T, kKeyNegInf);
     }
     const float theta = value_of(T);
 
-    // ---- sweep 2: the sum below theta and the candidates
+    // ---- sweep 2: the sum below theta and the candidates.  Each warp lists the chunks with an entry from theta
+    // on as it meets them and takes their entries afterwards, one a lane: the sum depends on no order
+    // but that of the row
     const float c = p.c;
     float S = 0.f;
-    unsigned long long fixed = 0ull;
     bool over = false;
-    auto append = [&](float v, int j) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < p.room) cand[at] = (static_cast<unsigned long long>(key_of(v)) << 32) | (0xffffffffu - static_cast<uint32_t>(j));
+    auto append = [&](bool is, float v, int j) {  // by whole warps
+        const unsigned m = __ballot_sync(0xffffffffu, is);
+        if (!m) return;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&sh.n, __popc(m));
+        at = __shfl_sync(0xffffffffu, at, 0) + __popc(m & ((1u << lane) - 1u));
+        if (is && at < p.room)
+            cand[at] = (static_cast<unsigned long long>(key_of(v)) << 32) | (0xffffffffu - static_cast<uint32_t>(j));
     };
     sweep([&](int n, int s0) {
-        if (tid == 0) sh.hits = 0;
-        __syncthreads();
         float2 acc = f2(0.f);
-#pragma unroll 2
-        for (int v = tid; v < n; v += kT) {
-            const uint4 r = lds_v4(staged + v * kW);
-            const bool hit = E::max_raw(r) >= theta;
+        int hits = 0;
+        auto chunk = [&](const uint4& r, int v, bool in) {
+            const bool hit = in && E::max_raw(r) >= theta;
             if constexpr (kRest) {
                 float2 d[kW / 2], e = f2(0.f);
                 E::minus(r, theta, d);
@@ -302,47 +369,67 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
                     const float2 a = mul2(d[i], f2(c));
                     e = add2(e, make_float2(ex2(a.x), ex2(a.y)));
                 }
-                acc = add2(acc, hit ? f2(0.f) : e);
+                acc = add2(acc, (hit || !in) ? f2(0.f) : e);
             }
-            if (hit) {
-                const int at = atomicAdd(&sh.hits, 1);
-                if (at < p.room) list[at] = static_cast<uint32_t>(v);
+            const unsigned m = __ballot_sync(0xffffffffu, hit);
+            if (m) {
+                const int at = hits + __popc(m & ((1u << lane) - 1u));
+                if (hit && at < list_room) list[at] = static_cast<unsigned short>(v);
+                hits += __popc(m);
             }
+        };
+        const uint4 none = ninf_raw<In>();
+        for (int v0 = warp * 32; v0 < n; v0 += 2 * kT) {
+            const int va = v0 + lane, vb = va + kT;
+            const uint4 ra = va < n ? lds_v4(staged + va * kW) : none, rb = vb < n ? lds_v4(staged + vb * kW) : none;
+            chunk(ra, va, va < n);
+            if (v0 + kT < n) chunk(rb, vb, vb < n);
         }
-        __syncthreads();
-        const int hits = sh.hits;
-        over |= hits > p.room;
+        __syncwarp();
+        over |= hits > list_room;
+        hits = min(hits, list_room);
         S += acc.x + acc.y;
-        for (int i = tid; i < min(hits, p.room) * kW; i += kT) {
-            const int at = static_cast<int>(list[i / kW]) * kW + i % kW;
+        for (int i0 = 0; i0 < hits * kW; i0 += 32) {
+            const int i = i0 + lane;
+            const bool in = i < hits * kW;
+            const int at = in ? static_cast<int>(list[i / kW]) * kW + i % kW : 0;
             const float v = E::lds(staged + at);
             const int j = s0 + at - ph;
-            if (v >= theta) {
-                if (j >= 0 && j < V) append(v, j);  // (-inf from outside the row)
-            } else if (kRest) {
-                fixed += __float2ull_rn(ex2((v - theta) * c) * kTopFix);
-            }
+            const bool is = in && v >= theta;
+            if (kRest && in && !is) S += ex2((v - theta) * c);
+            append(is && j >= 0 && j < V, v, j);  // (not the -inf from outside the row)
         }
-        __syncthreads();
+        __syncwarp();
     });
-    auto block_sum_fixed = [&](unsigned long long v) {
-        v = block_reduce<kT>(v, [](unsigned long long a, unsigned long long b) { return a + b; }, sh.warp_u);
-        return __ull2float_rn(v) * (1.f / kTopFix);
-    };
-    if constexpr (kRest) S = block_sum_f(S) + block_sum_fixed(fixed);
-    int n = sh.n;
-    TopPart part = {n, (over || n > p.room) ? 1 : 0, S, sh.err ? 1.f : 0.f};
-    const TopPart* parts = exchange(part);
-    int before = 0;
-    bool slow = false, err = false;
-    n = 0;
+    if constexpr (kRest) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+    }
+    if (lane == 0) {
+        sh.warp_f[warp] = S;
+        sh.warp_i[warp] = over ? 1 : 0;
+    }
+    __syncthreads();
+    int n = sh.n, before = 0;
+    bool slow = false, err = sh.err != 0;
     S = 0.f;
-    for (int r = 0; r < csize; ++r) {
-        before += r < rank ? parts[r].n : 0;
-        n += parts[r].n;
-        S += parts[r].s;
-        slow |= parts[r].m != 0;
-        err |= parts[r].top != 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        S += sh.warp_f[w];
+        slow |= sh.warp_i[w] != 0;
+    }
+    const TopPart* parts;
+    if (csize > 1) {
+        parts = exchange(TopPart{n, slow || n > p.room ? 1 : 0, S, err ? 1.f : 0.f});
+        n = 0;
+        S = 0.f;
+        for (int r = 0; r < csize; ++r) {
+            before += r < rank ? parts[r].n : 0;
+            n += parts[r].n;
+            S += parts[r].s;
+            slow |= parts[r].m != 0;
+            err |= parts[r].top != 0.f;
+        }
     }
     slow |= n > p.room;
     if (err) {  // a copy did not arrive in time
@@ -412,18 +499,19 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
                 if (count([at](uint32_t k) { return k >= at; }) >= K) kth = at;
             }
         }
+        T = kth;
         // the entries above it, then those equal to it, in index order: warps own runs of positions
         if (tid == 0) sh.n = 0;
         __syncthreads();
         int equal = 0;
         sweep([&](int nc, int s0) {
-            for (int i = tid; i < nc * kW; i += kT) {
-                const int j = s0 + i - ph;
-                if (j < 0 || j >= V) continue;
-                const float v = E::lds(staged + i);
+            for (int i0 = warp * 32; i0 < nc * kW; i0 += kT) {
+                const int i = i0 + lane, j = s0 + i - ph;
+                const bool in = i < nc * kW && j >= 0 && j < V;
+                const float v = in ? E::lds(staged + i) : 0.f;
                 const uint32_t k = key_of(v);
-                if (k > kth) append(v, j);
-                equal += k == kth ? 1 : 0;
+                append(in && k > kth, v, j);
+                equal += in && k == kth ? 1 : 0;
             }
         });
         __syncthreads();
@@ -457,7 +545,7 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
             for (int i = lo; i < hi && at < quota; i += 32) {
                 const bool eq = is(i + lane);
                 const unsigned m = __ballot_sync(0xffffffffu, eq);
-                if (eq && at + __popc(m & ((1u << lane) - 1u)) < quota) append(value_of(kth), s0 + i + lane - ph);
+                append(eq && at + __popc(m & ((1u << lane) - 1u)) < quota, value_of(kth), s0 + i + lane - ph);
                 at += __popc(m);
             }
             quota = max(0, quota - here);
@@ -495,65 +583,81 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
         if (rank > 0) return;
         cluster_wait();
     }
-    unsigned long long left = 0ull;
     auto emit = [&](unsigned long long k, int r) {
         if (r < K) {
             p.values[row * K + r] = value_of(static_cast<uint32_t>(k >> 32));
             p.ids[row * K + r] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(k));
+        } else if (r == K) {
+            sh.ref = value_of(static_cast<uint32_t>(k >> 32));
         }
     };
-    if (n <= kTopCountMost) {
-        constexpr int kPer = (kTopCountMost + kT - 1) / kT;
-        int r[kPer];
-        unsigned long long k[kPer];
+    // By the bin of each candidate's value; those of one bin compare with each other.  T and kmax bound the
+    // values, but for NaN, which goes to the last bin.
+    const uint32_t range = kmax > T ? kmax - T : 0u;
+    const int shift = shift_of(range);
+    auto bin_of = [&](unsigned long long k) {
+        const uint32_t v = static_cast<uint32_t>(k >> 32);
+        return static_cast<int>(min(v > T ? v - T : 0u, range) >> shift);
+    };
+    for (int i = tid; i < kTopBins; i += kT) sh.hist[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += kT) {
+        const unsigned long long k = cand[i];
+        sorted[i] = static_cast<unsigned long long>(atomicAdd(&sh.hist[bin_of(k)], 1));  // its place in the bin
+    }
+    __syncthreads();
+    if (warp == 0) scan_bins(K);
+    __syncthreads();
+    constexpr int kMostPer = 2048 / kT;  // candidates per thread: room <= 2048
+    int r[kMostPer];
+    if (sh.crowd <= kTopCrowd) {
+#pragma unroll
+        for (int u = 0; u < kMostPer; ++u) {
+            const int i = tid + u * kT;
+            if (i < n) r[u] = sh.base[bin_of(cand[i])] + static_cast<int>(sorted[i]);
+        }
         __syncthreads();
 #pragma unroll
-        for (int u = 0; u < kPer; ++u) {
+        for (int u = 0; u < kMostPer; ++u) {
             const int i = tid + u * kT;
-            r[u] = 0;
-            k[u] = i < n ? cand[i] : 0ull;
-            if (i - lane < n) {
-#pragma unroll 4
-                for (int j = 0; j < n; ++j) r[u] += cand[j] > k[u] ? 1 : 0;
-            }
-            if (i < n) {
-                emit(k[u], r[u]);
-                if (r[u] == K) sh.ref = value_of(static_cast<uint32_t>(k[u] >> 32));
-            }
+            if (i < n) sorted[r[u]] = cand[i];
         }
-        if (kRest && n > K) {
-            __syncthreads();
-            const float m = sh.ref;
+        __syncthreads();
 #pragma unroll
-            for (int u = 0; u < kPer; ++u)
-                if (tid + u * kT < n && r[u] >= K)
-                    left += __float2ull_rn(ex2((value_of(static_cast<uint32_t>(k[u] >> 32)) - m) * c) * kTopFix);
+        for (int u = 0; u < kMostPer; ++u) {
+            const int i = tid + u * kT;
+            if (i >= n) continue;
+            const unsigned long long k = sorted[i];
+            const int bin = bin_of(k), first = sh.base[bin], last = first + sh.hist[bin];
+            int at = first;
+            for (int j = first; j < last; ++j) at += sorted[j] > k ? 1 : 0;
+            emit(k, at);
+            r[u] = at;
         }
-    } else {
+    } else {  // many equal values: a bitonic sort
         int size = 1;
         while (size < n) size <<= 1;  // <= room
-        for (int i = n + tid; i < size; i += kT) cand[i] = 0ull;
+        for (int i = tid; i < size; i += kT) sorted[i] = i < n ? cand[i] : 0ull;
         for (int k = 2; k <= size; k <<= 1) {
             for (int j = k >> 1; j > 0; j >>= 1) {
                 __syncthreads();
                 for (int t = tid; t < size / 2; t += kT) {
                     const int a = 2 * t - (t & (j - 1)), b = a + j;
-                    const unsigned long long va = cand[a], vb = cand[b];
+                    const unsigned long long va = sorted[a], vb = sorted[b];
                     const bool descending = (a & k) == 0;
                     if ((va < vb) == descending) {
-                        cand[a] = vb;
-                        cand[b] = va;
+                        sorted[a] = vb;
+                        sorted[b] = va;
                     }
                 }
             }
         }
         __syncthreads();
-        for (int i = tid; i < min(n, K); i += kT) emit(cand[i], i);
-        if (kRest && n > K) {
-            const float m = value_of(static_cast<uint32_t>(cand[K] >> 32));
-            if (tid == 0) sh.ref = m;
-            for (int i = K + tid; i < n; i += kT)
-                left += __float2ull_rn(ex2((value_of(static_cast<uint32_t>(cand[i] >> 32)) - m) * c) * kTopFix);
+#pragma unroll
+        for (int u = 0; u < kMostPer; ++u) {
+            const int i = tid + u * kT;
+            r[u] = i;
+            if (i < n) emit(sorted[i], i);
         }
     }
     for (int i = n + tid; i < K; i += kT) {  // fewer than K numbers in the row
@@ -561,9 +665,17 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
         p.ids[row * K + i] = -1;
     }
     if constexpr (kRest) {
-        if (n > K) {
-            const float others = block_sum_fixed(left), m = sh.ref;
-            S = fmaf(S, ex2((ref - m) * c), others);
+        if (n > K) {  // the candidates that were not taken
+            __syncthreads();
+            const float m = sh.ref;
+#pragma unroll
+            for (int u = 0; u < kMostPer; ++u) {
+                const int i = tid + u * kT;
+                if (i < n && r[u] >= K)
+                    atomicAdd(&sh.left, __float2ull_rn(ex2((value_of(static_cast<uint32_t>(sorted[i] >> 32)) - m) * c) * kTopFix));
+            }
+            __syncthreads();
+            if (tid == 0) S = fmaf(S, ex2((ref - m) * c), __ull2float_rn(sh.left) * (1.f / kTopFix));
             ref = m;
         }
         if (tid == 0) p.rest[row] = S > 0.f ? fmaf(log2f(S), kLn2, __fdiv_rn(ref, p.tau)) : kNegInf;
@@ -572,7 +684,7 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
 
 // Shared memory per CTA beside the section.
 static size_t top_extra(int room, int csize, int groups) {
-    return size_t(room) * 12 + size_t(csize) * kTopThreads * groups * 4;
+    return size_t(room) * 20 + size_t(csize) * kTopThreads * groups * 4;
 }
 
 template <typename In>
