@@ -2,21 +2,23 @@
 // all other entries: the compact form in which the buffer R of Algorithm 1 keeps a
 // target row.
 //
-// One thread-block cluster per row, each CTA with its span of the row in shared memory
-// (one bulk copy), so that a row is read once:
+// One thread-block cluster per row, each CTA with a span of it that is read twice, the second time
+// from L2:
 //
-//   sweep 1  the maximum of each of several K groups of 16-byte chunks; the K-th
-//            largest of these, theta, found bit by bit, is reached by K entries at
-//            least, and by few more where large entries lie anyhow;
+//   sweep 1  the maximum of each of several K groups of 16-byte chunks; theta, which K of these
+//            reach and few more, from a histogram: K entries at least are theta or larger,
+//            and few more where large entries lie anyhow;
 //   sweep 2  the sum of the exponentials of the chunks below theta, and a list of the
 //            others, whose entries are then taken one by one: those from theta on are the
 //            candidates;
-//   finish   one CTA ranks the candidates (value, then index).  Those past the K-th join
-//            the sum.
+//   finish   one CTA ranks the candidates (value, then index) by a histogram of their values.
+//            Those past the K-th join the sum.
 //
 // Rows with more candidates than there is room for (many equal entries, or large ones
 // crowded in few groups) go on to the exact K-th largest value, counted bit by bit over the
-// staged row, and take the entries equal to it in index order.
+// row, and take the entries equal to it in index order.
+//
+// @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -30,17 +32,17 @@
 namespace osd {
 
 #ifndef TOPK_C
+#define TOPK_T 256
+#define TOPK_R 1280
 #define TOPK_C(bytes, rows) int((bytes + 72 * 1024 - 1) / (72 * 1024)) * (rows <= 152 ? 4 : 1)
 #endif
 
-constexpr int kTopThreads = 256;
 constexpr int kTopMaxCluster = 8;
 constexpr int kTopBins = 512;        // bins of a histogram over a range of keys
 constexpr int kTopCrowd = 48;        // candidates of one bin that are ranked by comparing; with more all are sorted
 // Exponentials (at most 1) of candidates, whose order is that of atomics, are added as whole multiples
 // of 2^-40, so that the sum does not depend on it.
 constexpr float kTopFix = 0x1p40f;
-constexpr uint64_t kTopWaitNs = 1000000000ull;  // bound on the wait for the bulk copies
 
 struct TopParams {
     const void* logits;
@@ -53,10 +55,8 @@ struct TopParams {
     float* values;
     int32_t* ids;
     float* rest;
-    int32_t* status;
     int csize;    // CTAs per row
     int span;     // positions per CTA: whole chunks
-    int section;  // positions staged at a time: the span, or what fits
     int room;     // candidates a CTA can hold, a power of two
     int groups;   // maxima per thread
 };
@@ -69,6 +69,7 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float value_of(uint32_t k) {
     return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
 }
+constexpr float kLn2Lo = -1.90465421e-9f;  // ln 2 - kLn2
 constexpr uint32_t kKeyNegInf = 0x007fffffu;
 
 // What the CTAs of a cluster tell each other at one point.
@@ -79,18 +80,22 @@ struct TopPart {
     float top;  // a maximum
 };
 
-struct TopSmem {
+// Where bin b lies: a lane of the scan reads 8 or 16 neighbouring bins, and the lanes' first ones
+// fall on different banks.
+__device__ __forceinline__ int top_slot(int b) { return b + (b >> 4); }
+
+template <int kWarps> struct TopSmem {
     TopPart parts[2][kTopMaxCluster];  // slot r from CTA r; alternately
     TopPart mine;
-    uint64_t bar;
-    int n, err, crowd;
+    int n, crowd;
+    uint32_t T, kmax;
     int bin, reach, above;  // of a histogram: the bin of the K-th largest, entries from it on, past it
     float ref;
     unsigned long long left;
-    int warp_i[kTopThreads / 32];
-    float warp_f[kTopThreads / 32];
-    uint32_t warp_hi[kTopThreads / 32], warp_lo[kTopThreads / 32];
-    __align__(16) int hist[kTopBins], base[kTopBins];  // entries per bin, and in the bins above it
+    int warp_i[kWarps];
+    float warp_f[kWarps];
+    uint32_t warp_hi[kWarps], warp_lo[kWarps];
+    int hist[kTopBins + 32], base[kTopBins + 32];  // entries per bin, and in the bins above it (at top_slot)
 };
 
 __device__ __forceinline__ void st_dsmem_v4(uint32_t addr, int a, int b, float c, float d) {
@@ -108,82 +113,54 @@ __device__ __forceinline__ void cluster_arrive_release() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
 
-template <typename In, bool kRest>
-__global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
+// Whether either half of a pair of bf16 numbers is at least that of another.
+__device__ __forceinline__ bool any_ge2(uint32_t a, uint32_t b) {
+    uint32_t ok;
+    asm("{\n .reg .pred p, q;\n setp.ge.bf16x2 p|q, %1, %2;\n or.pred p, p, q;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(a), "r"(b));
+    return ok != 0;
+}
+
+template <typename In, bool kRest, int kT>
+__global__ void __launch_bounds__(kT, TOPK_R / kT) topk_kernel(TopParams p) {
     using E = Elem<In>;
-    constexpr int kW = E::kVec, kT = kTopThreads, kWarps = kT / 32;
+    constexpr int kW = E::kVec, kWarps = kT / 32;
     extern __shared__ __align__(128) unsigned char dsm[];
-    __shared__ __align__(16) TopSmem sh;
+    __shared__ __align__(16) TopSmem<kWarps> sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int csize = p.csize, rank = csize > 1 ? static_cast<int>(cluster_rank()) : 0;
-    const long long row = blockIdx.x / csize;
+    const unsigned row = csize > 1 ? blockIdx.x / static_cast<unsigned>(csize) : blockIdx.x;
     const int V = p.V, K = p.K;
-    if (tid == 0) mbar_init(&sh.bar, 1);
     grid_dependency_sync();
     if (p.mask && !p.mask[row]) return;  // the cluster alike
     if (csize > 1) cluster_arrive_relaxed();  // (no CTA writes to one that has not started)
-    const In* x = static_cast<const In*>(p.logits) + (row / p.P) * p.sg + (row % p.P) * p.sp;
+    unsigned group = row, pos = 0;
+    if (p.P > 1) {
+        group = row / static_cast<unsigned>(p.P);
+        pos = row - group * static_cast<unsigned>(p.P);
+    }
+    const In* x = static_cast<const In*>(p.logits) + group * p.sg + pos * p.sp;
+    float* values = p.values + size_t(row) * K;
+    int32_t* ids = p.ids + size_t(row) * K;
     // entry j counts as position j + ph: chunks of positions are 16-byte vectors of the row
     const int ph = static_cast<int>((reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(In));
-    const int p0 = rank * p.span, p1 = min(p0 + p.span, V + ph);  // this CTA's positions
-    In* staged = reinterpret_cast<In*>(dsm);
-    unsigned long long* cand = reinterpret_cast<unsigned long long*>(dsm + size_t(p.section) * sizeof(In));
+    const int p0 = rank * p.span, p1 = min(p0 + p.span, V + ph);  // this CTA's positions,
+    const int first = max(p0 - ph, 0), end = max(first, p1 - ph); // its entries,
+    const int c0 = (first + ph + kW - 1) / kW, c1 = max(c0, (end + ph) / kW);  // its whole chunks [c0, c1),
+    const int head = min(end, c0 * kW - ph), tail = min(end, max(head, c1 * kW - ph));  // and the entries before and after them
+    const int singles = (head - first) + (end - tail);
+    const In* body = x - ph;  // chunk v starts at body + v kW
+    unsigned long long* cand = reinterpret_cast<unsigned long long*>(dsm);
     unsigned long long* sorted = cand + p.room;
-    // chunks with an entry from theta on, a part for every warp
-    const int list_room = p.room / 4;
-    unsigned short* list = reinterpret_cast<unsigned short*>(sorted + p.room) + warp * list_room;
-    uint32_t* maxima = reinterpret_cast<uint32_t*>(sorted + p.room) + p.room;
-    const int sections = max(1, (p1 - p0 + p.section - 1) / p.section);  // (a CTA past the row's end has an empty one)
-    unsigned parity = 0;
+    // chunks with an entry from theta on, a part for every warp; later the candidates' places
+    const int list_room = 2 * p.room / kWarps;
+    uint32_t* lists = reinterpret_cast<uint32_t*>(sorted + p.room);
+    uint32_t* list = lists + warp * list_room;
+    uint32_t* maxima = lists + 2 * p.room;
     if (tid == 0) {
-        sh.err = 0;
         sh.n = 0;
         sh.left = 0ull;
     }
-    __syncthreads();
-
-    // Positions [s0, s0 + section) of this CTA into shared memory; what lies outside the row reads as -inf.
-    // Returns the number of chunks.
-    auto stage = [&](int sec) -> int {
-        const int s0 = p0 + sec * p.section, s1 = min(s0 + p.section, p1);
-        const int n = max(0, (s1 - s0 + kW - 1) / kW);
-        const int c0 = s0 < ph ? 1 : 0;                                   // whole chunks [c0, c1)
-        const int c1 = max(c0, (s0 + n * kW > V + ph) ? n - 1 : n);
-        if (tid == 0 && c1 > c0) {
-            const uint32_t bytes = static_cast<uint32_t>(c1 - c0) * 16u;
-            mbar_arrive_expect_tx(&sh.bar, bytes);
-            bulk_g2s(staged + c0 * kW, x + (s0 + c0 * kW - ph), bytes, &sh.bar);
-        }
-        for (int i = tid; i < n * kW; i += kT) {
-            if (i >= c0 * kW && i < c1 * kW) {  // on to the last chunk
-                i += ((c1 * kW - i + kT - 1) / kT) * kT - kT;
-                continue;
-            }
-            const int j = s0 + i - ph;
-            E::store(staged + i, j >= 0 && j < V ? E::load(x + j) : kNegInf);
-        }
-        if (c1 > c0) {
-            if (!mbar_wait_bounded(&sh.bar, parity, kTopWaitNs)) {
-                sh.err = 1;
-                mbar_wait_bounded(&sh.bar, parity, kTopWaitNs);  // give the copy in flight a last chance to land
-            }
-            parity ^= 1u;
-        }
-        __syncthreads();
-        return n;
-    };
-    int chunks = stage(0);
-    // f(chunks, first position) on each section in turn; the only one stays staged
-    auto sweep = [&](auto&& f) {
-        for (int sec = 0; sec < sections; ++sec) {
-            if (sections > 1) {
-                fence_proxy_async_smem();  // (the accesses of the section before)
-                __syncthreads();
-                chunks = stage(sec);
-            }
-            f(chunks, p0 + sec * p.section);
-        }
-    };
+    auto single = [&](int i) { return i < head - first ? first + i : tail + (i - (head - first)); };
     unsigned turn = 0;
     // this CTA's part (thread 0's) to every CTA of the cluster; the parts are in the result for every thread
     auto exchange = [&](TopPart mine) -> const TopPart* {
@@ -205,36 +182,46 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
         cluster_wait();
         return slots;
     };
-    auto block_sum_f = [&](float v) {
-        return block_reduce<kT>(v, [](float a, float b) { return a + b; }, sh.warp_f);
-    };
-    auto block_max_f = [&](float v) {
-        return block_reduce<kT>(v, [](float a, float b) { return fmaxf(a, b); }, sh.warp_f);
-    };
-    auto block_sum_i = [&](int v) { return block_reduce<kT>(v, [](int a, int b) { return a + b; }, sh.warp_i); };
 
+    // the larger of each word of two chunks (bf16: of each half)
+    auto max_into = [](uint4& a, const uint4& b) {
+        if constexpr (sizeof(In) == 2) {
+            a = make_uint4(bmax2(a.x, b.x), bmax2(a.y, b.y), bmax2(a.z, b.z), bmax2(a.w, b.w));
+        } else {
+            a = make_uint4(__float_as_uint(fmaxf(__uint_as_float(a.x), __uint_as_float(b.x))),
+                           __float_as_uint(fmaxf(__uint_as_float(a.y), __uint_as_float(b.y))),
+                           __float_as_uint(fmaxf(__uint_as_float(a.z), __uint_as_float(b.z))),
+                           __float_as_uint(fmaxf(__uint_as_float(a.w), __uint_as_float(b.w))));
+        }
+    };
     // ---- sweep 1: group maxima of all CTAs, into every CTA
     const int g = p.groups, mine_at = rank * kT * g;
-    for (int i = tid; i < kT * g; i += kT) maxima[mine_at + i] = 0u;
-    sweep([&](int n, int) {
-        for (int k = 0; k < g; ++k) {
-            float m = kNegInf;
-            const int first = tid + k * kT, step = kT * g;
-            int v = first;
-            for (; v + 3 * step < n; v += 4 * step) {  // (four loads in flight)
-                uint4 r[4];
+    for (int k = 0; k < g; ++k) {
+        const int step = kT * g, at = c0 + tid + k * kT;
+        uint4 m = ninf_raw<In>();
+        int v = at;
+        for (; v + 3 * step < c1; v += 4 * step) {  // (four loads in flight)
+            uint4 r[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) r[i] = lds_v4(staged + (v + i * step) * kW);
+            for (int i = 0; i < 4; ++i) r[i] = ldg_stream(body + size_t(v + i * step) * kW);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) m = fmaxf(m, E::max_raw(r[i]));
-            }
-            for (; v < n; v += step) m = fmaxf(m, E::max_raw(lds_v4(staged + v * kW)));
-            if (first < n) {
-                uint32_t& at = maxima[mine_at + first];
-                at = max(at, key_of(m));
-            }
+            for (int i = 0; i < 4; ++i) max_into(m, r[i]);
         }
-    });
+        if (v < c1) {
+            uint4 r[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = ldg_stream(body + size_t(min(v + i * step, c1 - 1)) * kW);  // (the last again)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) max_into(m, v + i * step < c1 ? r[i] : m);
+        }
+        float top = E::max_raw(m);
+        bool any = at < c1;
+        if (k == 0 && tid < singles) {
+            top = fmaxf(top, E::load(x + single(tid)));
+            any = true;
+        }
+        maxima[mine_at + k * kT + tid] = any ? key_of(top) : 0u;
+    }
     if (csize > 1) {
         cluster_wait();
         for (int i = tid; i < kT * g; i += kT) {
@@ -246,45 +233,29 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
         cluster_wait();
     }
     const int total = kT * g * csize;
-    uint32_t kmax, kmin;  // the largest, and the smallest of a group that has entries
-    {
-        uint32_t hi = 0u, lo = 0xffffffffu;
-        for (int i = tid; i < total; i += kT) {
-            const uint32_t k = maxima[i];
-            hi = max(hi, k);
-            if (k) lo = min(lo, k);
-        }
-        hi = __reduce_max_sync(0xffffffffu, hi);
-        lo = __reduce_min_sync(0xffffffffu, lo);
-        if (lane == 0) {
-            sh.warp_hi[warp] = hi;
-            sh.warp_lo[warp] = lo;
-        }
-        for (int i = tid; i < kTopBins; i += kT) sh.hist[i] = 0;
-        __syncthreads();
-        kmax = sh.warp_hi[0];
-        kmin = sh.warp_lo[0];
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) {
-            kmax = max(kmax, sh.warp_hi[w]);
-            kmin = min(kmin, sh.warp_lo[w]);
-        }
-    }
-    auto shift_of = [](uint32_t range) { return max(0, 32 - __clz(range) - 9); };  // range >> it < 512 bins
-    // warp 0: from the histogram, the entries in the bins above each (base), the highest bin from which on there are
-    // `need`, and the fullest bin
-    auto scan_bins = [&](int need) {
-        constexpr int kPer = kTopBins / 32;
-        int h[kPer], sum = 0, most = 0;
-#pragma unroll
-        for (int i = 0; i < kPer; i += 4) {
-            const int4 v = *reinterpret_cast<const int4*>(&sh.hist[lane * kPer + i]);
-            h[i] = v.x; h[i + 1] = v.y; h[i + 2] = v.z; h[i + 3] = v.w;
-        }
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            sum += h[i];
-            most = max(most, h[i]);
+    // 2^bits bins over a range of keys
+    const int bits = K <= 128 ? 8 : 9;
+    auto shift_of = [bits](uint32_t range) { return max(0, 32 - __clz(range) - bits); };
+    // The two histograms are the work of a team: one warp where it has little to do (the others would spend as
+    // many instructions on nothing), else the whole CTA.
+    auto team_sync = [&](auto all) {
+        if constexpr (decltype(all)::value) __syncthreads();
+        else __syncwarp();
+    };
+    auto clear_bins = [&](auto all) {
+        constexpr bool kAll = decltype(all)::value;
+        for (int i = kAll ? tid : lane; i < top_slot(1 << bits); i += kAll ? kT : 32) sh.hist[i] = 0;
+    };
+    // one warp: from the histogram the highest bin from which on there are `need` entries, and, where wanted, the
+    // entries in the bins above each and the fullest bin
+    auto scan_bins = [&](int need, auto bases) {
+        constexpr bool kBases = decltype(bases)::value;
+        const int per = (1 << bits) / 32;
+        int sum = 0, most = 0;
+        for (int i = 0; i < per; ++i) {
+            const int h = sh.hist[top_slot(lane * per + i)];
+            sum += h;
+            most = max(most, h);
         }
         int incl = sum;  // of this lane's bins and all above
 #pragma unroll
@@ -292,135 +263,197 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
             const int y = __shfl_down_sync(0xffffffffu, incl, o);
             if (lane + o < 32) incl += y;
         }
-        int above = incl - sum, bin = -1, reach = 0, past = 0;
-#pragma unroll
-        for (int i = kPer - 1; i >= 0; --i) {
-            sh.base[lane * kPer + i] = above;
-            if (above < need && above + h[i] >= need) {
-                bin = lane * kPer + i;
-                reach = above + h[i];
-                past = above;
+        int above = incl - sum;
+        const bool mine = above < need && incl >= need;
+        if (kBases || mine) {
+            for (int i = per - 1; i >= 0; --i) {
+                const int at = top_slot(lane * per + i), h = sh.hist[at];
+                if constexpr (kBases) sh.base[at] = above;
+                if (above < need && above + h >= need) {
+                    sh.bin = lane * per + i;
+                    sh.reach = above + h;
+                    sh.above = above;
+                }
+                above += h;
             }
-            above += h[i];
         }
-        most = __reduce_max_sync(0xffffffffu, most);
-        const unsigned has = __ballot_sync(0xffffffffu, bin >= 0);
-        if (lane == (has ? __ffs(has) - 1 : 0)) {
-            sh.bin = bin;
-            sh.reach = reach;
-            sh.above = past;
-            sh.crowd = most;
+        if constexpr (kBases) {
+            most = __reduce_max_sync(0xffffffffu, most);
+            if (lane == 0) sh.crowd = most;
+        } else {
+            if (!__any_sync(0xffffffffu, mine) && lane == 0) sh.bin = -1;
         }
     };
     // T: reached by K maxima or more, and by few more, from a histogram over the range of the maxima, refined in
     // the bin of the K-th largest where that holds many (a row with a few entries far above the others)
-    uint32_t T = 0u;
-    {
-        uint32_t lo = kmin, hi = kmax;
+    auto find_theta = [&](auto all) {
+        constexpr bool kAll = decltype(all)::value;
+        const int t0 = kAll ? tid : lane, step = kAll ? kT : 32;
+        uint32_t hi = 0u, lo = 0xffffffffu, T = 0u;  // the largest, and the smallest of a group that has entries
+        for (int i = t0; i < total; i += step) {
+            const uint32_t k = maxima[i];
+            hi = max(hi, k);
+            if (k) lo = min(lo, k);
+        }
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        clear_bins(all);
+        if constexpr (kAll) {
+            if (lane == 0) {
+                sh.warp_hi[warp] = hi;
+                sh.warp_lo[warp] = lo;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                hi = max(hi, sh.warp_hi[w]);
+                lo = min(lo, sh.warp_lo[w]);
+            }
+        } else {
+            __syncwarp();
+        }
+        if (kAll ? tid == 0 : lane == 0) sh.kmax = hi;
         int above = 0;
         while (lo <= hi) {
             const int shift = shift_of(hi - lo);
-            for (int i = tid; i < total; i += kT) {
+            for (int i = t0; i < total; i += step) {
                 const uint32_t k = maxima[i];
-                if (k >= lo && k <= hi) atomicAdd(&sh.hist[(k - lo) >> shift], 1);
+                if (k >= lo && k <= hi) atomicAdd(&sh.hist[top_slot(static_cast<int>((k - lo) >> shift))], 1);
             }
-            __syncthreads();
-            if (warp == 0) scan_bins(K - above);
-            __syncthreads();
-            const int bin = sh.bin;
+            team_sync(all);
+            if (!kAll || warp == 0) scan_bins(K - above, std::false_type());
+            team_sync(all);
+            const int bin = sh.bin, reach = sh.reach, past = sh.above;
             if (bin < 0) break;  // fewer than K groups
             T = lo + (static_cast<uint32_t>(bin) << shift);
-            if (above + sh.reach <= K + K / 8 + 4 || shift == 0) break;
-            above += sh.above;
+            if (above + reach <= K + K / 8 + 4 || shift == 0) break;
+            above += past;
             lo = T;
             hi = min(hi, T + ((1u << shift) - 1u));
-            for (int i = tid; i < kTopBins; i += kT) sh.hist[i] = 0;
-            __syncthreads();
+            clear_bins(all);
+            team_sync(all);
         }
-        T = max(T, kKeyNegInf);
+        return max(T, kKeyNegInf);
+    };
+    uint32_t T;
+    if (total <= 512) {
+        __syncthreads();
+        if (warp == 0) {
+            T = find_theta(std::false_type());
+            if (lane == 0) sh.T = T;
+        }
+        __syncthreads();
+        T = sh.T;
+    } else {
+        T = find_theta(std::true_type());
     }
     const float theta = value_of(T);
 
     // ---- sweep 2: the sum below theta and the candidates.  Each warp lists the chunks with an entry from theta
     // on as it meets them and takes their entries afterwards, one a lane: the sum depends on no order
     // but that of the row
-    const float c = p.c;
+    // (exponents x c - M as one FMA, M = rn(theta c): one rounding, after the cancellation, and M belongs to the
+    // sum.  They stay below 1: x < theta)
+    const float c = p.c, M = theta == kNegInf ? 0.f : __fmul_rn(theta, c);
     float S = 0.f;
     bool over = false;
-    auto append = [&](bool is, float v, int j) {  // by whole warps
-        const unsigned m = __ballot_sync(0xffffffffu, is);
-        if (!m) return;
-        int at = 0;
-        if (lane == 0) at = atomicAdd(&sh.n, __popc(m));
-        at = __shfl_sync(0xffffffffu, at, 0) + __popc(m & ((1u << lane) - 1u));
-        if (is && at < p.room)
+    auto append = [&](float v, int j) {
+        const int at = atomicAdd(&sh.n, 1);
+        if (at < p.room)
             cand[at] = (static_cast<unsigned long long>(key_of(v)) << 32) | (0xffffffffu - static_cast<uint32_t>(j));
     };
-    sweep([&](int n, int s0) {
+    // whether a chunk has an entry from theta on (bf16: packed, theta rounded up to the entries' grid)
+    const uint32_t theta2 = __byte_perm(__float_as_uint(theta < 0.f ? theta : __uint_as_float((__float_as_uint(theta) + 0xffffu) & 0xffff0000u)), 0u, 0x3232);
+    auto reaches = [&](const uint4& r) {
+        if constexpr (sizeof(In) == 2) {
+            const uint32_t m = bmax2(bmax2(r.x, r.y), bmax2(r.z, r.w));
+            return any_ge2(m, theta2);
+        } else {
+            return E::max_raw(r) >= theta;
+        }
+    };
+    {
         float2 acc = f2(0.f);
         int hits = 0;
-        auto chunk = [&](const uint4& r, int v, bool in) {
-            const bool hit = in && E::max_raw(r) >= theta;
+        auto chunk = [&](const uint4& raw, int v, auto whole) {
+            const bool in = decltype(whole)::value || v < c1, hit = in && reaches(raw);
             if constexpr (kRest) {
-                float2 d[kW / 2], e = f2(0.f);
-                E::minus(r, theta, d);
+                float y[kW];
+                E::unpack(raw, y);
+                float2 d[kW / 2];
 #pragma unroll
-                for (int i = 0; i < kW / 2; ++i) {
-                    const float2 a = mul2(d[i], f2(c));
-                    e = add2(e, make_float2(ex2(a.x), ex2(a.y)));
+                for (int e = 0; e < kW / 2; ++e) {
+                    const float2 a = fma2(make_float2(y[2 * e], y[2 * e + 1]), f2(c), f2(-M));
+                    d[e] = make_float2(ex2(a.x), ex2(a.y));
                 }
-                acc = add2(acc, (hit || !in) ? f2(0.f) : e);
+#pragma unroll
+                for (int w = kW / 4; w > 0; w /= 2)
+#pragma unroll
+                    for (int e = 0; e < w; ++e) d[e] = add2(d[e], d[e + w]);
+                if (in && !hit) acc = add2(acc, d[0]);
             }
             const unsigned m = __ballot_sync(0xffffffffu, hit);
             if (m) {
                 const int at = hits + __popc(m & ((1u << lane) - 1u));
-                if (hit && at < list_room) list[at] = static_cast<unsigned short>(v);
+                if (hit && at < list_room) list[at] = static_cast<uint32_t>(v);
                 hits += __popc(m);
             }
         };
-        const uint4 none = ninf_raw<In>();
-        for (int v0 = warp * 32; v0 < n; v0 += 2 * kT) {
-            const int va = v0 + lane, vb = va + kT;
-            const uint4 ra = va < n ? lds_v4(staged + va * kW) : none, rb = vb < n ? lds_v4(staged + vb * kW) : none;
-            chunk(ra, va, va < n);
-            if (v0 + kT < n) chunk(rb, vb, vb < n);
+        int v0 = c0 + warp * 32;
+        for (; v0 + 3 * kT + 32 <= c1; v0 += 4 * kT) {  // (four loads in flight)
+            uint4 raw[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw[i] = ldg_stream(body + size_t(v0 + i * kT + lane) * kW);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) chunk(raw[i], v0 + i * kT + lane, std::true_type());
+        }
+        if (v0 < c1) {
+            uint4 raw[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw[i] = ldg_stream(body + size_t(min(v0 + i * kT + lane, c1 - 1)) * kW);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (v0 + i * kT < c1) chunk(raw[i], v0 + i * kT + lane, std::false_type());
         }
         __syncwarp();
         over |= hits > list_room;
         hits = min(hits, list_room);
         S += acc.x + acc.y;
-        for (int i0 = 0; i0 < hits * kW; i0 += 32) {
-            const int i = i0 + lane;
-            const bool in = i < hits * kW;
-            const int at = in ? static_cast<int>(list[i / kW]) * kW + i % kW : 0;
-            const float v = E::lds(staged + at);
-            const int j = s0 + at - ph;
-            const bool is = in && v >= theta;
-            if (kRest && in && !is) S += ex2((v - theta) * c);
-            append(is && j >= 0 && j < V, v, j);  // (not the -inf from outside the row)
+        // a listed chunk a lane, then, in the first warp, the single entries
+        for (int i = lane; i < hits; i += 32) {
+            const int v = static_cast<int>(list[i]);
+            float y[kW];
+            E::unpack(ldg_stream(body + size_t(v) * kW), y);
+#pragma unroll
+            for (int e = 0; e < kW; ++e) {
+                if (y[e] >= theta) append(y[e], v * kW + e - ph);
+                else if (kRest) S += ex2(fmaf(y[e], c, -M));
+            }
         }
-        __syncwarp();
-    });
+        if (warp == 0 && lane < singles) {
+            const int j = single(lane);
+            const float v = E::load(x + j);
+            if (v >= theta) append(v, j);
+            else if (kRest) S += ex2(fmaf(v, c, -M));
+        }
+    }
     if constexpr (kRest) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
     }
     if (lane == 0) {
         sh.warp_f[warp] = S;
-        sh.warp_i[warp] = over ? 1 : 0;
+        if (over) atomicAdd(&sh.n, 1 << 24);  // (above any room)
     }
     __syncthreads();
     int n = sh.n, before = 0;
-    bool slow = false, err = sh.err != 0;
-    S = 0.f;
+    bool slow = n > p.room;
+    S = sh.warp_f[0];
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        S += sh.warp_f[w];
-        slow |= sh.warp_i[w] != 0;
-    }
+    for (int w = 1; w < kWarps; ++w) S += sh.warp_f[w];
     const TopPart* parts;
     if (csize > 1) {
-        parts = exchange(TopPart{n, slow || n > p.room ? 1 : 0, S, err ? 1.f : 0.f});
+        parts = exchange(TopPart{min(n, 1 << 24), slow ? 1 : 0, S, 0.f});
         n = 0;
         S = 0.f;
         for (int r = 0; r < csize; ++r) {
@@ -428,62 +461,44 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
             n += parts[r].n;
             S += parts[r].s;
             slow |= parts[r].m != 0;
-            err |= parts[r].top != 0.f;
         }
     }
     slow |= n > p.room;
-    if (err) {  // a copy did not arrive in time
-        if (rank == 0) {
-            for (int i = tid; i < K; i += kT) {
-                p.values[row * K + i] = kNegInf;
-                p.ids[row * K + i] = -1;
-            }
-            if (tid == 0) {
-                if (p.rest) p.rest[row] = kNegInf;
-                if (p.status) atomicExch(p.status, static_cast<int32_t>(OSD_ERR_TIMEOUT));
-            }
-        }
-        return;
-    }
-    float ref = theta;
-    // the largest entry below `bound` and the sum of 2^((x - it) c) of all entries below, over the cluster
-    auto below = [&](float bound, float& m, float& s) {
+    float log_ref = mul_c(M, kLn2, kLn2Lo);  // the logarithm of what the sum is against
+    // the sum of the entries' exponentials below `bound` over the cluster, against the largest of them, m
+    auto below = [&](float bound, float& m) {
         float mx = kNegInf;
-        sweep([&](int nc, int) {
-            for (int i = tid; i < nc * kW; i += kT) {
-                const float v = E::lds(staged + i);
-                if (v < bound) mx = fmaxf(mx, v);
-            }
-        });
-        mx = block_max_f(mx);
+#pragma unroll 8
+        for (int j = first + tid; j < end; j += kT) {
+            const float v = E::load(x + j);
+            if (v < bound) mx = fmaxf(mx, v);
+        }
+        mx = block_reduce<kT>(mx, [](float a, float b) { return fmaxf(a, b); }, sh.warp_f);
         const TopPart* q = exchange(TopPart{0, 0, 0.f, mx});
         for (int r = 0; r < csize; ++r) mx = fmaxf(mx, q[r].top);
         float sum = 0.f;
-        if (mx != kNegInf)
-            sweep([&](int nc, int) {
-                for (int i = tid; i < nc * kW; i += kT) {
-                    const float v = E::lds(staged + i);
-                    if (v < bound) sum += ex2((v - mx) * c);
-                }
-            });
-        sum = block_sum_f(sum);
+        if (mx != kNegInf) {
+#pragma unroll 8
+            for (int j = first + tid; j < end; j += kT) {
+                const float v = E::load(x + j);
+                if (v < bound) sum += ex2((v - mx) * c);
+            }
+        }
+        sum = block_reduce<kT>(sum, [](float a, float b) { return a + b; }, sh.warp_f);
         q = exchange(TopPart{0, 0, sum, 0.f});
+        m = mx;
         sum = 0.f;
         for (int r = 0; r < csize; ++r) sum += q[r].s;
-        m = mx;
-        s = sum;
+        return sum;
     };
     if (slow) {
         // the exact K-th largest key: theta itself if fewer than K entries lie above it
+        auto block_sum = [&](int v) { return block_reduce<kT>(v, [](int a, int b) { return a + b; }, sh.warp_i); };
         auto count = [&](auto pred) {
             int m = 0;
-            sweep([&](int nc, int s0) {
-                for (int i = tid; i < nc * kW; i += kT) {
-                    const int j = s0 + i - ph;
-                    m += (j >= 0 && j < V && pred(key_of(E::lds(staged + i)))) ? 1 : 0;
-                }
-            });
-            m = block_sum_i(m);
+#pragma unroll 8
+            for (int j = first + tid; j < end; j += kT) m += pred(key_of(E::load(x + j))) ? 1 : 0;
+            m = block_sum(m);
             const TopPart* q = exchange(TopPart{m, 0, 0.f, 0.f});
             m = 0;
             for (int r = 0; r < csize; ++r) m += q[r].n;
@@ -500,57 +515,47 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
             }
         }
         T = kth;
-        // the entries above it, then those equal to it, in index order: warps own runs of positions
+        // the entries above it, then those equal to it, in index order: warps own runs of entries
         if (tid == 0) sh.n = 0;
         __syncthreads();
         int equal = 0;
-        sweep([&](int nc, int s0) {
-            for (int i0 = warp * 32; i0 < nc * kW; i0 += kT) {
-                const int i = i0 + lane, j = s0 + i - ph;
-                const bool in = i < nc * kW && j >= 0 && j < V;
-                const float v = in ? E::lds(staged + i) : 0.f;
-                const uint32_t k = key_of(v);
-                append(in && k > kth, v, j);
-                equal += in && k == kth ? 1 : 0;
-            }
-        });
+        for (int j0 = first + warp * 32; j0 < end; j0 += kT) {
+            const bool in = j0 + lane < end;
+            const float v = in ? E::load(x + j0 + lane) : 0.f;
+            const uint32_t k = key_of(v);
+            if (in && k > kth) append(v, j0 + lane);
+            equal += in && k == kth ? 1 : 0;
+        }
         __syncthreads();
         const int above = min(sh.n, p.room);
-        equal = block_sum_i(equal);
+        equal = block_sum(equal);
         parts = exchange(TopPart{above, equal, 0.f, 0.f});
-        int first = 0, all_above = 0, all_equal = 0;  // equal entries in lower CTAs
+        int lower = 0, all_above = 0, all_equal = 0;  // equal entries in lower CTAs
         for (int r = 0; r < csize; ++r) {
-            first += r < rank ? parts[r].m : 0;
+            lower += r < rank ? parts[r].m : 0;
             all_above += parts[r].n;
             all_equal += parts[r].m;
         }
-        int quota = max(0, min(equal, K - all_above - first));  // how many of the equal ones here are taken
-        sweep([&](int nc, int s0) {
-            const int per = (nc * kW + kWarps * 32 - 1) / (kWarps * 32) * 32;
-            const int lo = min(nc * kW, warp * per), hi = min(nc * kW, lo + per);
-            auto is = [&](int i) {
-                const int j = s0 + i - ph;
-                return i < hi && j >= 0 && j < V && key_of(E::lds(staged + i)) == kth;
-            };
+        const int quota = max(0, min(equal, K - all_above - lower));  // how many of the equal ones here are taken
+        {
+            const int per = ((end - first + kWarps - 1) / kWarps + 31) / 32 * 32;
+            const int lo = min(end, first + warp * per), hi = min(end, lo + per);
+            auto is = [&](int j) { return j < hi && key_of(E::load(x + j)) == kth; };
             int mine = 0;
-            for (int i = lo; i < hi; i += 32) mine += __popc(__ballot_sync(0xffffffffu, is(i + lane)));
+            for (int j = lo; j < hi; j += 32) mine += __popc(__ballot_sync(0xffffffffu, is(j + lane)));
             __syncthreads();
             if (lane == 0) sh.warp_i[warp] = mine;
             __syncthreads();
-            int at = 0, here = 0;
-            for (int w = 0; w < kWarps; ++w) {
-                at += w < warp ? sh.warp_i[w] : 0;
-                here += sh.warp_i[w];
-            }
-            for (int i = lo; i < hi && at < quota; i += 32) {
-                const bool eq = is(i + lane);
+            int at = 0;
+            for (int w = 0; w < warp; ++w) at += sh.warp_i[w];
+            for (int j = lo; j < hi && at < quota; j += 32) {
+                const bool eq = is(j + lane);
                 const unsigned m = __ballot_sync(0xffffffffu, eq);
-                append(eq && at + __popc(m & ((1u << lane) - 1u)) < quota, value_of(kth), s0 + i + lane - ph);
+                if (eq && at + __popc(m & ((1u << lane) - 1u)) < quota) append(value_of(kth), j + lane);
                 at += __popc(m);
             }
-            quota = max(0, quota - here);
             __syncthreads();
-        });
+        }
         n = min(sh.n, p.room);
         parts = exchange(TopPart{n, 0, 0.f, 0.f});
         before = n = 0;
@@ -561,16 +566,18 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
         if constexpr (kRest) {
             const float v = value_of(kth);
             float m;
-            below(v, m, S);
+            S = below(v, m);
             const int left = all_above + all_equal - K;  // equal entries that were not taken
-            ref = m;
             if (left > 0 && v != kNegInf) {
-                S = (m == kNegInf ? 0.f : S * ex2((m - v) * c)) + static_cast<float>(left);
-                ref = v;
+                S = (S > 0.f ? S * ex2((m - v) * c) : 0.f) + static_cast<float>(left);
+                m = v;
             }
+            log_ref = __fdiv_rn(m, p.tau);
         }
-    } else if (kRest && n <= K && !(S > 0x1p-10f)) {
-        below(theta, ref, S);  // all others lie below theta by far: their sum against their own largest
+    } else if (kRest && n <= K && !(S > 0x1p-10f)) {  // all others lie below theta by far
+        float m;
+        S = below(theta, m);
+        log_ref = __fdiv_rn(m, p.tau);
     }
     // ---- finish: all candidates to the first CTA
     n = min(n, p.room);
@@ -583,136 +590,133 @@ __global__ void __launch_bounds__(kTopThreads, 3) topk_kernel(TopParams p) {
         if (rank > 0) return;
         cluster_wait();
     }
-    auto emit = [&](unsigned long long k, int r) {
-        if (r < K) {
-            p.values[row * K + r] = value_of(static_cast<uint32_t>(k >> 32));
-            p.ids[row * K + r] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(k));
-        } else if (r == K) {
-            sh.ref = value_of(static_cast<uint32_t>(k >> 32));
-        }
-    };
-    // By the bin of each candidate's value; those of one bin compare with each other.  T and kmax bound the
-    // values, but for NaN, which goes to the last bin.
-    const uint32_t range = kmax > T ? kmax - T : 0u;
+    // By the bin of each candidate's value; those of one bin compare with each other.  T and the largest maximum
+    // bound the values, but for NaN, which goes to the last bin.
+    const uint32_t range = sh.kmax > T ? sh.kmax - T : 0u;
     const int shift = shift_of(range);
     auto bin_of = [&](unsigned long long k) {
         const uint32_t v = static_cast<uint32_t>(k >> 32);
-        return static_cast<int>(min(v > T ? v - T : 0u, range) >> shift);
+        return top_slot(static_cast<int>(min(v > T ? v - T : 0u, range) >> shift));
     };
-    for (int i = tid; i < kTopBins; i += kT) sh.hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += kT) {
-        const unsigned long long k = cand[i];
-        sorted[i] = static_cast<unsigned long long>(atomicAdd(&sh.hist[bin_of(k)], 1));  // its place in the bin
-    }
-    __syncthreads();
-    if (warp == 0) scan_bins(K);
-    __syncthreads();
-    constexpr int kMostPer = 2048 / kT;  // candidates per thread: room <= 2048
-    int r[kMostPer];
-    if (sh.crowd <= kTopCrowd) {
-#pragma unroll
-        for (int u = 0; u < kMostPer; ++u) {
-            const int i = tid + u * kT;
-            if (i < n) r[u] = sh.base[bin_of(cand[i])] + static_cast<int>(sorted[i]);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < kMostPer; ++u) {
-            const int i = tid + u * kT;
-            if (i < n) sorted[r[u]] = cand[i];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < kMostPer; ++u) {
-            const int i = tid + u * kT;
-            if (i >= n) continue;
-            const unsigned long long k = sorted[i];
-            const int bin = bin_of(k), first = sh.base[bin], last = first + sh.hist[bin];
-            int at = first;
-            for (int j = first; j < last; ++j) at += sorted[j] > k ? 1 : 0;
-            emit(k, at);
-            r[u] = at;
-        }
-    } else {  // many equal values: a bitonic sort
-        int size = 1;
-        while (size < n) size <<= 1;  // <= room
-        for (int i = tid; i < size; i += kT) sorted[i] = i < n ? cand[i] : 0ull;
-        for (int k = 2; k <= size; k <<= 1) {
-            for (int j = k >> 1; j > 0; j >>= 1) {
-                __syncthreads();
-                for (int t = tid; t < size / 2; t += kT) {
-                    const int a = 2 * t - (t & (j - 1)), b = a + j;
-                    const unsigned long long va = sorted[a], vb = sorted[b];
-                    const bool descending = (a & k) == 0;
-                    if ((va < vb) == descending) {
-                        sorted[a] = vb;
-                        sorted[b] = va;
+    unsigned short* place = reinterpret_cast<unsigned short*>(lists);
+    auto finish = [&](auto all) {
+        constexpr bool kAll = decltype(all)::value;
+        const int t0 = kAll ? tid : lane, step = kAll ? kT : 32;
+        auto emit = [&](unsigned long long k, int r) {
+            if (r < K) {
+                values[r] = value_of(static_cast<uint32_t>(k >> 32));
+                ids[r] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(k));
+            } else if (r == K) {
+                sh.ref = value_of(static_cast<uint32_t>(k >> 32));
+            }
+        };
+        clear_bins(all);
+        team_sync(all);
+        for (int i = t0; i < n; i += step)
+            place[i] = static_cast<unsigned short>(atomicAdd(&sh.hist[bin_of(cand[i])], 1));  // in its bin
+        team_sync(all);
+        if (!kAll || warp == 0) scan_bins(K, std::true_type());
+        team_sync(all);
+        if (sh.crowd <= kTopCrowd) {
+            for (int i = t0; i < n; i += step) sorted[sh.base[bin_of(cand[i])] + place[i]] = cand[i];
+            team_sync(all);
+            for (int i = t0; i < n; i += step) {
+                const unsigned long long k = sorted[i];
+                const int slot = bin_of(k), from = sh.base[slot], to = from + sh.hist[slot];
+                int at = from;
+                for (int j = from; j < to; ++j) at += sorted[j] > k ? 1 : 0;
+                emit(k, at);
+                place[i] = static_cast<unsigned short>(at);
+            }
+        } else {  // many equal values: a bitonic sort
+            int size = 1;
+            while (size < n) size <<= 1;  // <= room
+            for (int i = t0; i < size; i += step) sorted[i] = i < n ? cand[i] : 0ull;
+            for (int k = 2; k <= size; k <<= 1) {
+                for (int j = k >> 1; j > 0; j >>= 1) {
+                    team_sync(all);
+                    for (int t = t0; t < size / 2; t += step) {
+                        const int a = 2 * t - (t & (j - 1)), b = a + j;
+                        const unsigned long long va = sorted[a], vb = sorted[b];
+                        const bool descending = (a & k) == 0;
+                        if ((va < vb) == descending) {
+                            sorted[a] = vb;
+                            sorted[b] = va;
+                        }
                     }
                 }
             }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < kMostPer; ++u) {
-            const int i = tid + u * kT;
-            r[u] = i;
-            if (i < n) emit(sorted[i], i);
-        }
-    }
-    for (int i = n + tid; i < K; i += kT) {  // fewer than K numbers in the row
-        p.values[row * K + i] = kNegInf;
-        p.ids[row * K + i] = -1;
-    }
-    if constexpr (kRest) {
-        if (n > K) {  // the candidates that were not taken
-            __syncthreads();
-            const float m = sh.ref;
-#pragma unroll
-            for (int u = 0; u < kMostPer; ++u) {
-                const int i = tid + u * kT;
-                if (i < n && r[u] >= K)
-                    atomicAdd(&sh.left, __float2ull_rn(ex2((value_of(static_cast<uint32_t>(sorted[i] >> 32)) - m) * c) * kTopFix));
+            team_sync(all);
+            for (int i = t0; i < n; i += step) {
+                emit(sorted[i], i);
+                place[i] = static_cast<unsigned short>(i);
             }
-            __syncthreads();
-            if (tid == 0) S = fmaf(S, ex2((ref - m) * c), __ull2float_rn(sh.left) * (1.f / kTopFix));
-            ref = m;
         }
-        if (tid == 0) p.rest[row] = S > 0.f ? fmaf(log2f(S), kLn2, __fdiv_rn(ref, p.tau)) : kNegInf;
+        for (int i = n + t0; i < K; i += step) {  // fewer than K numbers in the row
+            values[i] = kNegInf;
+            ids[i] = -1;
+        }
+        if constexpr (kRest) {
+            if (n > K) {  // the candidates that were not taken, against the largest of them
+                team_sync(all);
+                const float v = sh.ref;
+                unsigned long long left = 0ull;
+                for (int i = t0; i < n; i += step)
+                    if (place[i] >= K)
+                        left += __float2ull_rn(ex2((value_of(static_cast<uint32_t>(sorted[i] >> 32)) - v) * c) * kTopFix);
+                if (__any_sync(0xffffffffu, left != 0ull)) {
+                    left = warp_sum_u64(left);
+                    if (kAll && lane == 0) atomicAdd(&sh.left, left);
+                }
+                if constexpr (kAll) {
+                    __syncthreads();
+                    left = sh.left;
+                }
+                S = (S > 0.f ? S * ex2(fmaf(-v, c, M)) : 0.f) + __ull2float_rn(left) * (1.f / kTopFix);
+                log_ref = __fdiv_rn(v, p.tau);
+            }
+            if (t0 == 0) p.rest[row] = S > 0.f ? fmaf(log2f(S), kLn2, log_ref) : kNegInf;
+        }
+    };
+    if (n <= 128) {
+        __syncthreads();
+        if (warp == 0) finish(std::false_type());
+    } else {
+        finish(std::true_type());
     }
 }
 
-// Shared memory per CTA beside the section.
-static size_t top_extra(int room, int csize, int groups) {
-    return size_t(room) * 20 + size_t(csize) * kTopThreads * groups * 4;
-}
-
-template <typename In>
-static osd_status launch_topk(TopParams tp, long long rows, cudaStream_t s) {
+template <typename In, int kT>
+static osd_status launch_topk(TopParams tp, long long rows, int c, cudaStream_t s) {
     constexpr int kW = Elem<In>::kVec;
-    constexpr size_t es = sizeof(In);
-    constexpr size_t kMost = 200 * 1024;
     const int positions = tp.V + kW - 1;  // a row starts up to kW - 1 positions into the grid
-    const long long bytes = (long long)positions * (long long)es;
-    int c = TOPK_C(bytes, rows);
     c = std::max(1, std::min(c, kTopMaxCluster));
     tp.span = ((positions + c - 1) / c + 63) / 64 * 64;
     tp.csize = (positions + tp.span - 1) / tp.span;
     tp.room = 256;
     while (tp.room < tp.K + tp.K / 2 + 128) tp.room *= 2;
-    const int per = (tp.span / kW + kTopThreads - 1) / kTopThreads;  // chunks per thread
-    tp.groups = std::max(1, std::min(per, (4 * tp.K + tp.csize * kTopThreads - 1) / (tp.csize * kTopThreads)));
-    const size_t extra = top_extra(tp.room, tp.csize, tp.groups);
-    tp.section = static_cast<int>(std::min<size_t>(tp.span, (kMost - extra) / es / 64 * 64));
-    const size_t smem = size_t(tp.section) * es + extra;
+    const int per = (tp.span / kW + kT - 1) / kT;  // chunks per thread
+    tp.groups = std::max(1, std::min(per, (4 * tp.K + tp.csize * kT - 1) / (tp.csize * kT)));
+    const size_t smem = size_t(tp.room) * 24 + size_t(tp.csize) * kT * tp.groups * 4;
     if (rows * tp.csize > INT_MAX) return OSD_ERR_UNSUPPORTED;
     auto go = [&](auto kernel_tag) -> osd_status {
         constexpr bool kRest = decltype(kernel_tag)::value;
-        if (ctas_per_sm<topk_kernel<In, kRest>, kTopThreads>(smem) < 1) return OSD_ERR_CUDA;  // (opts in for the size)
-        return from_cuda(launch_ex(true, topk_kernel<In, kRest>, dim3(static_cast<unsigned>(rows * tp.csize)), dim3(kTopThreads),
+        if (ctas_per_sm<topk_kernel<In, kRest, kT>, kT>(smem) < 1) return OSD_ERR_CUDA;  // (opts in for the size)
+        return from_cuda(launch_ex(true, topk_kernel<In, kRest, kT>, dim3(static_cast<unsigned>(rows * tp.csize)), dim3(kT),
                                    smem, s, tp.csize, tp));
     };
     return tp.rest ? go(std::true_type()) : go(std::false_type());
+}
+
+template <typename In>
+static osd_status launch_topk_dtype(const TopParams& tp, long long rows, cudaStream_t s) {
+    const long long bytes = (long long)tp.V * (long long)sizeof(In);
+    const int c = TOPK_C(bytes, rows);
+    switch (TOPK_T) {
+        case 128: return launch_topk<In, 128>(tp, rows, c, s);
+        case 256: return launch_topk<In, 256>(tp, rows, c, s);
+        default: return launch_topk<In, 512>(tp, rows, c, s);
+    }
 }
 
 }  // namespace osd
@@ -741,6 +745,6 @@ extern "C" osd_status osd_topk(const void* logits, osd_dtype dtype, int G, int P
     tp.logits = logits; tp.P = P; tp.V = V; tp.sg = stride_g; tp.sp = stride_p; tp.mask = mask; tp.K = K;
     tp.c = static_cast<float>(1.4426950408889634074 / static_cast<double>(temperature));
     tp.tau = temperature;
-    tp.values = values; tp.ids = ids; tp.rest = rest; tp.status = status;
-    return dtype == OSD_BF16 ? launch_topk<__nv_bfloat16>(tp, rows, s) : launch_topk<float>(tp, rows, s);
+    tp.values = values; tp.ids = ids; tp.rest = rest;
+    return dtype == OSD_BF16 ? launch_topk_dtype<__nv_bfloat16>(tp, rows, s) : launch_topk_dtype<float>(tp, rows, s);
 }
