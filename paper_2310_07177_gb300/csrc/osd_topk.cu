@@ -2,21 +2,21 @@
 // all other entries: the compact form in which the buffer R of Algorithm 1 keeps a
 // target row.
 //
-// One thread-block cluster per row, each CTA with a span of it that is read twice, the second time
-// from L2:
+// One thread-block cluster per row, which is read once but for a few groups of entries:
 //
-//   sweep 1  the maximum of each of several K groups of 16-byte chunks; theta, which K of these
-//            reach and few more, from a histogram: K entries at least are theta or larger,
-//            and few more where large entries lie anyhow;
-//   sweep 2  the sum of the exponentials of the chunks below theta, and a list of the
-//            others, whose entries are then taken one by one: those from theta on are the
-//            candidates;
-//   finish   one CTA ranks the candidates (value, then index) by a histogram of their values.
-//            Those past the K-th join the sum.
+//   sweep    every thread takes eight groups of 16-byte chunks and keeps each group's
+//            maximum and sum of exponentials;
+//   theta    a value that K group maxima reach and few more, from a histogram of them: at
+//            least K entries are theta or larger, and few more where large entries lie
+//            anyhow.  Groups below theta are done: their sums count.  The others are
+//            read again (from L2) and taken entry by entry: entries below theta join the sum,
+//            the others are the candidates;
+//   finish   one CTA ranks the candidates (value, then index).  Those past the K-th join
+//            the sum.
 //
 // Rows with more candidates than there is room for (many equal entries, or large ones
-// crowded in few groups) go on to the exact K-th largest value, counted bit by bit over the
-// row, and take the entries equal to it in index order.
+// crowded in few groups) go on to the exact K-th largest value, from histograms of all entries,
+// and take the entries equal to it in index order.
 //
 // @@
 #include <algorithm>
@@ -31,18 +31,16 @@
 
 namespace osd {
 
-#ifndef TOPK_C
-#define TOPK_T 256
-#define TOPK_R 1280
-#define TOPK_C(bytes, rows) int((bytes + 72 * 1024 - 1) / (72 * 1024)) * (rows <= 152 ? 4 : 1)
-#endif
-
 constexpr int kTopMaxCluster = 8;
-constexpr int kTopBins = 512;        // bins of a histogram over a range of keys
+constexpr int kTopGroups = 8;        // groups of chunks per thread
+constexpr int kTopBins = 256;        // bins of a histogram over a range of keys
+constexpr int kTopCountMost = 192;   // candidates ranked by counting; more by a histogram of their values
 constexpr int kTopCrowd = 48;        // candidates of one bin that are ranked by comparing; with more all are sorted
 // Exponentials (at most 1) of candidates, whose order is that of atomics, are added as whole multiples
 // of 2^-40, so that the sum does not depend on it.
 constexpr float kTopFix = 0x1p40f;
+constexpr float kLn2Lo = -1.90465421e-9f;  // ln 2 - kLn2
+constexpr uint32_t kKeyNegInf = 0x007fffffu;
 
 struct TopParams {
     const void* logits;
@@ -55,10 +53,10 @@ struct TopParams {
     float* values;
     int32_t* ids;
     float* rest;
-    int csize;    // CTAs per row
-    int span;     // positions per CTA: whole chunks
-    int room;     // candidates a CTA can hold, a power of two
-    int groups;   // maxima per thread
+    int csize;   // CTAs per row
+    int span;    // positions per CTA: whole chunks
+    int room;    // candidates a CTA can hold, a power of two
+    int maxima;  // maxima per thread that theta is found from: 1, 2, 4 or 8
 };
 
 // Unsigned keys in the order of the floats; -0 and 0 have the same.
@@ -69,8 +67,11 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float value_of(uint32_t k) {
     return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
 }
-constexpr float kLn2Lo = -1.90465421e-9f;  // ln 2 - kLn2
-constexpr uint32_t kKeyNegInf = 0x007fffffu;
+// A candidate: its key, and its index so that of equal values the lower index is the larger number.
+__device__ __forceinline__ unsigned long long cand_of(float x, int j) {
+    return (static_cast<unsigned long long>(key_of(x)) << 32) | (0xffffffffu - static_cast<uint32_t>(j));
+}
+__device__ __forceinline__ float cand_value(unsigned long long k) { return value_of(static_cast<uint32_t>(k >> 32)); }
 
 // What the CTAs of a cluster tell each other at one point.
 struct TopPart {
@@ -80,22 +81,18 @@ struct TopPart {
     float top;  // a maximum
 };
 
-// Where bin b lies: a lane of the scan reads 8 or 16 neighbouring bins, and the lanes' first ones
-// fall on different banks.
-__device__ __forceinline__ int top_slot(int b) { return b + (b >> 4); }
-
 template <int kWarps> struct TopSmem {
     TopPart parts[2][kTopMaxCluster];  // slot r from CTA r; alternately
     TopPart mine;
+    __align__(16) int hist[kTopBins];  // entries per bin,
+    __align__(16) int base[kTopBins];  // and in the bins above it
     int n, crowd;
-    uint32_t T, kmax;
     int bin, reach, above;  // of a histogram: the bin of the K-th largest, entries from it on, past it
     float ref;
     unsigned long long left;
     int warp_i[kWarps];
     float warp_f[kWarps];
     uint32_t warp_hi[kWarps], warp_lo[kWarps];
-    int hist[kTopBins + 32], base[kTopBins + 32];  // entries per bin, and in the bins above it (at top_slot)
 };
 
 __device__ __forceinline__ void st_dsmem_v4(uint32_t addr, int a, int b, float c, float d) {
@@ -108,22 +105,31 @@ __device__ __forceinline__ void st_dsmem_u32(uint32_t addr, uint32_t v) {
 __device__ __forceinline__ void st_dsmem_u64(uint32_t addr, unsigned long long v) {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
 }
+__device__ __forceinline__ void add_dsmem_s32(uint32_t addr, int v) {
+    asm volatile("red.shared::cluster.add.s32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
 __device__ __forceinline__ void cluster_arrive_release() {
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
 
-// Whether either half of a pair of bf16 numbers is at least that of another.
-__device__ __forceinline__ bool any_ge2(uint32_t a, uint32_t b) {
-    uint32_t ok;
-    asm("{\n .reg .pred p, q;\n setp.ge.bf16x2 p|q, %1, %2;\n or.pred p, p, q;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(a), "r"(b));
-    return ok != 0;
-}
+// The largest entries of two chunks, in as few words as the type allows (bf16: one of a pair).
+template <typename In> struct ChunkMax;
+template <> struct ChunkMax<float> {
+    float m = kNegInf;
+    __device__ __forceinline__ void add(const uint4& r) { m = fmaxf(m, Elem<float>::max_raw(r)); }
+    __device__ __forceinline__ float top() const { return m; }
+};
+template <> struct ChunkMax<__nv_bfloat16> {
+    uint32_t m = 0xFF80FF80u;
+    __device__ __forceinline__ void add(const uint4& r) { m = bmax2(m, bmax2(bmax2(r.x, r.y), bmax2(r.z, r.w))); }
+    __device__ __forceinline__ float top() const { return fmaxf(bf16_lo(m), bf16_hi(m)); }
+};
 
 template <typename In, bool kRest, int kT>
-__global__ void __launch_bounds__(kT, TOPK_R / kT) topk_kernel(TopParams p) {
+__global__ void __launch_bounds__(kT, 1024 / kT) topk_kernel(TopParams p) {
     using E = Elem<In>;
-    constexpr int kW = E::kVec, kWarps = kT / 32;
+    constexpr int kW = E::kVec, kWarps = kT / 32, kG = kTopGroups;
     extern __shared__ __align__(128) unsigned char dsm[];
     __shared__ __align__(16) TopSmem<kWarps> sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -146,21 +152,245 @@ __global__ void __launch_bounds__(kT, TOPK_R / kT) topk_kernel(TopParams p) {
     const int p0 = rank * p.span, p1 = min(p0 + p.span, V + ph);  // this CTA's positions,
     const int first = max(p0 - ph, 0), end = max(first, p1 - ph); // its entries,
     const int c0 = (first + ph + kW - 1) / kW, c1 = max(c0, (end + ph) / kW);  // its whole chunks [c0, c1),
-    const int head = min(end, c0 * kW - ph), tail = min(end, max(head, c1 * kW - ph));  // and the entries before and after them
-    const int singles = (head - first) + (end - tail);
+    const int head = min(end, c0 * kW - ph), tail = min(end, max(head, c1 * kW - ph));  // and the entries before and
+    const int singles = (head - first) + (end - tail);                                  // after them
     const In* body = x - ph;  // chunk v starts at body + v kW
+    auto single = [&](int i) { return i < head - first ? first + i : tail + (i - (head - first)); };
+    auto load = [&](int v) { return ldg_stream(body + size_t(v) * kW); };
     unsigned long long* cand = reinterpret_cast<unsigned long long*>(dsm);
     unsigned long long* sorted = cand + p.room;
-    // chunks with an entry from theta on, a part for every warp; later the candidates' places
-    const int list_room = 2 * p.room / kWarps;
-    uint32_t* lists = reinterpret_cast<uint32_t*>(sorted + p.room);
-    uint32_t* list = lists + warp * list_room;
-    uint32_t* maxima = lists + 2 * p.room;
+    uint32_t* maxima = reinterpret_cast<uint32_t*>(sorted + p.room);
+    unsigned short* place = reinterpret_cast<unsigned short*>(maxima + csize * kT * p.maxima);
+    unsigned char* list = reinterpret_cast<unsigned char*>(place + p.room) + warp * (32 * kG);
     if (tid == 0) {
         sh.n = 0;
         sh.left = 0ull;
     }
-    auto single = [&](int i) { return i < head - first ? first + i : tail + (i - (head - first)); };
+    for (int i = tid; i < kTopBins; i += kT) sh.hist[i] = 0;
+
+    // ---- sweep: group i of a thread holds its chunks i, i + kG, ... ; sums are against M, from the thread's
+    // first chunk
+    const float c = p.c;
+    ChunkMax<In> gmax[kG];
+    float gsum[kG], M = 0.f;
+#pragma unroll
+    for (int i = 0; i < kG; ++i) gsum[i] = 0.f;
+    auto exps = [&](const uint4& raw, float m) {  // the sum of 2^(x c - m) of a chunk
+        float y[kW];
+        E::unpack(raw, y);
+        float2 d[kW / 2];
+#pragma unroll
+        for (int e = 0; e < kW / 2; ++e) {
+            const float2 a = fma2(make_float2(y[2 * e], y[2 * e + 1]), f2(c), f2(-m));
+            d[e] = make_float2(ex2(a.x), ex2(a.y));
+        }
+#pragma unroll
+        for (int w = kW / 4; w > 0; w /= 2)
+#pragma unroll
+            for (int e = 0; e < w; ++e) d[e] = add2(d[e], d[e + w]);
+        return d[0].x + d[0].y;
+    };
+    const int v0 = c0 + tid;
+    constexpr int kHalf = kG / 2;
+    for (int v = v0; v < c1; v += kG * kT) {
+#pragma unroll
+        for (int h = 0; h < kG; h += kHalf) {
+            const int vh = v + h * kT;
+            uint4 raw[kHalf];
+            if (vh + (kHalf - 1) * kT < c1) {
+#pragma unroll
+                for (int i = 0; i < kHalf; ++i) raw[i] = load(vh + i * kT);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kHalf; ++i) {
+                    raw[i] = ninf_raw<In>();
+                    if (vh + i * kT < c1) raw[i] = load(vh + i * kT);
+                }
+            }
+            if (kRest && h == 0 && v == v0) {
+                const float m = E::max_raw(raw[0]);
+                M = m == kNegInf ? 0.f : __fmul_rn(m, c);
+            }
+#pragma unroll
+            for (int i = 0; i < kHalf; ++i) {
+                gmax[h + i].add(raw[i]);
+                if constexpr (kRest) gsum[h + i] += exps(raw[i], M);
+            }
+        }
+    }
+
+    // ---- theta: from p.maxima maxima per thread, of all CTAs in every CTA
+    const int per = p.maxima, mine_at = rank * kT * per;
+    if (csize > 1) cluster_wait();
+    {
+        // (maximum i of a thread is that of its groups i, i + per, ... : short rows fill the first of them)
+        float top[kG];
+#pragma unroll
+        for (int i = 0; i < kG; ++i) top[i] = gmax[i].top();
+        bool any = v0 < c1;
+        if (tid < singles) {
+            top[0] = fmaxf(top[0], E::load(x + single(tid)));
+            any = true;
+        }
+#pragma unroll
+        for (int w = kG / 2; w > 0; w /= 2)
+            if (per <= w)
+#pragma unroll
+                for (int i = 0; i < w; ++i) top[i] = fmaxf(top[i], top[i + w]);
+#pragma unroll
+        for (int i = 0; i < kG; ++i) {
+            if (i >= per) break;
+            const uint32_t k = (i == 0 ? any : v0 + i * kT < c1) ? key_of(top[i]) : 0u;
+            const int at = mine_at + i * kT + tid;
+            maxima[at] = k;
+            for (int r = 0; csize > 1 && r < csize; ++r)
+                if (r != rank) st_dsmem_u32(map_rank(&maxima[at], static_cast<uint32_t>(r)), k);
+        }
+    }
+    if (csize > 1) {
+        cluster_arrive_release();
+        cluster_wait();
+    }
+    const int total = kT * per * csize;
+    auto shift_of = [](uint32_t range) { return max(0, 24 - __clz(range)); };  // range >> it < kTopBins
+    // warp 0: from the histogram the highest bin from which on there are `need` entries, and, where wanted, the
+    // entries in the bins above each and the fullest bin
+    auto scan_bins = [&](int need, auto bases) {
+        constexpr int kPer = kTopBins / 32;
+        const int4 a = reinterpret_cast<const int4*>(sh.hist)[2 * lane], b = reinterpret_cast<const int4*>(sh.hist)[2 * lane + 1];
+        const int h[kPer] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        int from[kPer + 1];  // entries from bin i of this lane's on, in it and in the lanes above
+        from[kPer] = 0;
+#pragma unroll
+        for (int i = kPer - 1; i >= 0; --i) from[i] = from[i + 1] + h[i];
+        int incl = from[0];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_down_sync(0xffffffffu, incl, o);
+            if (lane + o < 32) incl += y;
+        }
+        const int above = incl - from[0];
+        if constexpr (decltype(bases)::value) {
+            reinterpret_cast<int4*>(sh.base)[2 * lane] =
+                make_int4(above + from[1], above + from[2], above + from[3], above + from[4]);
+            reinterpret_cast<int4*>(sh.base)[2 * lane + 1] =
+                make_int4(above + from[5], above + from[6], above + from[7], above);
+            int most = h[0];
+#pragma unroll
+            for (int i = 1; i < kPer; ++i) most = max(most, h[i]);
+            most = __reduce_max_sync(0xffffffffu, most);
+            if (lane == 0) sh.crowd = most;
+        } else {
+            if (above < need && incl >= need) {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    if (above + from[i + 1] < need && above + from[i] >= need) {
+                        sh.bin = lane * kPer + i;
+                        sh.reach = above + from[i];
+                        sh.above = above + from[i + 1];
+                    }
+            }
+            if (incl < need && lane == 0) sh.bin = -1;  // fewer than that in all
+        }
+    };
+    // T: reached by K maxima or more, and by few more, from a histogram over the range of the maxima, refined in
+    // the bin of the K-th largest where that holds many (a row with a few entries far above the others)
+    uint32_t T = 0u, kmax = 0u;
+    {
+        uint32_t lo = 0xffffffffu;  // the smallest of a group that has entries
+        for (int i = tid; i < total; i += kT) {
+            const uint32_t k = maxima[i];
+            kmax = max(kmax, k);
+            if (k) lo = min(lo, k);
+        }
+        kmax = __reduce_max_sync(0xffffffffu, kmax);
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        if (lane == 0) {
+            sh.warp_hi[warp] = kmax;
+            sh.warp_lo[warp] = lo;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            kmax = max(kmax, sh.warp_hi[w]);
+            lo = min(lo, sh.warp_lo[w]);
+        }
+        uint32_t hi = kmax;
+        int above = 0;
+        while (lo <= hi) {
+            const int shift = shift_of(hi - lo);
+            for (int i = tid; i < total; i += kT) {
+                const uint32_t k = maxima[i];
+                if (k >= lo && k <= hi) atomicAdd(&sh.hist[(k - lo) >> shift], 1);
+            }
+            __syncthreads();
+            if (warp == 0) scan_bins(K - above, std::false_type());
+            __syncthreads();
+            const int bin = sh.bin, reach = sh.reach, past = sh.above;
+            if (bin < 0) break;  // fewer than K groups
+            T = lo + (static_cast<uint32_t>(bin) << shift);
+            if (above + reach <= K + K / 8 + 4 || shift == 0) break;
+            above += past;
+            lo = T;
+            hi = min(hi, T + ((1u << shift) - 1u));
+            for (int i = tid; i < kTopBins; i += kT) sh.hist[i] = 0;
+            __syncthreads();
+        }
+        T = max(T, kKeyNegInf);
+    }
+    const float theta = value_of(T);
+
+    // ---- the groups below theta, and the entries of the others.  (Exponents x c - Mt as one FMA, Mt = rn(theta c):
+    // one rounding, after the cancellation, and Mt belongs to the sum; they stay below 1, as x < theta.)  A group
+    // whose thread took its first chunk from far above theta, or whose sum is near overflow, is taken by entries
+    // too.  A warp lists its groups in one order, so that the sum depends on none.
+    const float Mt = theta == kNegInf ? 0.f : __fmul_rn(theta, c);
+    float S = 0.f;
+    auto append = [&](float v, int j) {
+        const int at = atomicAdd(&sh.n, 1);
+        if (at < p.room) cand[at] = cand_of(v, j);
+    };
+    {
+        const bool far = kRest && !(M - Mt <= 20.f);
+        const float scale = far ? 0.f : ex2(M - Mt);
+        int hits = 0;
+#pragma unroll
+        for (int i = 0; i < kG; ++i) {
+            const bool is = v0 + i * kT < c1 && (gmax[i].top() >= theta || far || (kRest && !(gsum[i] < 0x1p100f)));
+            if (kRest && !is) S = fmaf(gsum[i], scale, S);
+            const unsigned m = __ballot_sync(0xffffffffu, is);
+            if (is) list[hits + __popc(m & ((1u << lane) - 1u))] = static_cast<unsigned char>(lane * kG + i);
+            hits += __popc(m);
+        }
+        __syncwarp();
+        auto entry = [&](float y, int j) {
+            if (y >= theta) append(y, j);
+            else if (kRest) S += ex2(fmaf(y, c, -Mt));
+        };
+        for (int i = lane; i < hits; i += 32) {
+            const int at = list[i];
+            for (int v = c0 + warp * 32 + at / kG + (at % kG) * kT; v < c1; v += kG * kT) {
+                float y[kW];
+                E::unpack(load(v), y);
+#pragma unroll
+                for (int e = 0; e < kW; ++e) entry(y[e], v * kW + e - ph);
+            }
+        }
+        if (tid < singles) entry(E::load(x + single(tid)), single(tid));
+    }
+    if constexpr (kRest) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+        if (lane == 0) sh.warp_f[warp] = S;
+    }
+    __syncthreads();
+    int n = sh.n, before = 0;
+    bool slow = n > p.room;
+    if constexpr (kRest) {
+        S = sh.warp_f[0];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) S += sh.warp_f[w];
+    }
     unsigned turn = 0;
     // this CTA's part (thread 0's) to every CTA of the cluster; the parts are in the result for every thread
     auto exchange = [&](TopPart mine) -> const TopPart* {
@@ -182,289 +412,19 @@ __global__ void __launch_bounds__(kT, TOPK_R / kT) topk_kernel(TopParams p) {
         cluster_wait();
         return slots;
     };
-
-    // the larger of each word of two chunks (bf16: of each half)
-    auto max_into = [](uint4& a, const uint4& b) {
-        if constexpr (sizeof(In) == 2) {
-            a = make_uint4(bmax2(a.x, b.x), bmax2(a.y, b.y), bmax2(a.z, b.z), bmax2(a.w, b.w));
-        } else {
-            a = make_uint4(__float_as_uint(fmaxf(__uint_as_float(a.x), __uint_as_float(b.x))),
-                           __float_as_uint(fmaxf(__uint_as_float(a.y), __uint_as_float(b.y))),
-                           __float_as_uint(fmaxf(__uint_as_float(a.z), __uint_as_float(b.z))),
-                           __float_as_uint(fmaxf(__uint_as_float(a.w), __uint_as_float(b.w))));
-        }
-    };
-    // ---- sweep 1: group maxima of all CTAs, into every CTA
-    const int g = p.groups, mine_at = rank * kT * g;
-    for (int k = 0; k < g; ++k) {
-        const int step = kT * g, at = c0 + tid + k * kT;
-        uint4 m = ninf_raw<In>();
-        int v = at;
-        for (; v + 3 * step < c1; v += 4 * step) {  // (four loads in flight)
-            uint4 r[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = ldg_stream(body + size_t(v + i * step) * kW);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) max_into(m, r[i]);
-        }
-        if (v < c1) {
-            uint4 r[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = ldg_stream(body + size_t(min(v + i * step, c1 - 1)) * kW);  // (the last again)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) max_into(m, v + i * step < c1 ? r[i] : m);
-        }
-        float top = E::max_raw(m);
-        bool any = at < c1;
-        if (k == 0 && tid < singles) {
-            top = fmaxf(top, E::load(x + single(tid)));
-            any = true;
-        }
-        maxima[mine_at + k * kT + tid] = any ? key_of(top) : 0u;
-    }
-    if (csize > 1) {
-        cluster_wait();
-        for (int i = tid; i < kT * g; i += kT) {
-            const uint32_t v = maxima[mine_at + i];
-            for (int r = 0; r < csize; ++r)
-                if (r != rank) st_dsmem_u32(map_rank(&maxima[mine_at + i], static_cast<uint32_t>(r)), v);
-        }
-        cluster_arrive_release();
-        cluster_wait();
-    }
-    const int total = kT * g * csize;
-    // 2^bits bins over a range of keys
-    const int bits = K <= 128 ? 8 : 9;
-    auto shift_of = [bits](uint32_t range) { return max(0, 32 - __clz(range) - bits); };
-    // The two histograms are the work of a team: one warp where it has little to do (the others would spend as
-    // many instructions on nothing), else the whole CTA.
-    auto team_sync = [&](auto all) {
-        if constexpr (decltype(all)::value) __syncthreads();
-        else __syncwarp();
-    };
-    auto clear_bins = [&](auto all) {
-        constexpr bool kAll = decltype(all)::value;
-        for (int i = kAll ? tid : lane; i < top_slot(1 << bits); i += kAll ? kT : 32) sh.hist[i] = 0;
-    };
-    // one warp: from the histogram the highest bin from which on there are `need` entries, and, where wanted, the
-    // entries in the bins above each and the fullest bin
-    auto scan_bins = [&](int need, auto bases) {
-        constexpr bool kBases = decltype(bases)::value;
-        const int per = (1 << bits) / 32;
-        int sum = 0, most = 0;
-        for (int i = 0; i < per; ++i) {
-            const int h = sh.hist[top_slot(lane * per + i)];
-            sum += h;
-            most = max(most, h);
-        }
-        int incl = sum;  // of this lane's bins and all above
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_down_sync(0xffffffffu, incl, o);
-            if (lane + o < 32) incl += y;
-        }
-        int above = incl - sum;
-        const bool mine = above < need && incl >= need;
-        if (kBases || mine) {
-            for (int i = per - 1; i >= 0; --i) {
-                const int at = top_slot(lane * per + i), h = sh.hist[at];
-                if constexpr (kBases) sh.base[at] = above;
-                if (above < need && above + h >= need) {
-                    sh.bin = lane * per + i;
-                    sh.reach = above + h;
-                    sh.above = above;
-                }
-                above += h;
-            }
-        }
-        if constexpr (kBases) {
-            most = __reduce_max_sync(0xffffffffu, most);
-            if (lane == 0) sh.crowd = most;
-        } else {
-            if (!__any_sync(0xffffffffu, mine) && lane == 0) sh.bin = -1;
-        }
-    };
-    // T: reached by K maxima or more, and by few more, from a histogram over the range of the maxima, refined in
-    // the bin of the K-th largest where that holds many (a row with a few entries far above the others)
-    auto find_theta = [&](auto all) {
-        constexpr bool kAll = decltype(all)::value;
-        const int t0 = kAll ? tid : lane, step = kAll ? kT : 32;
-        uint32_t hi = 0u, lo = 0xffffffffu, T = 0u;  // the largest, and the smallest of a group that has entries
-        for (int i = t0; i < total; i += step) {
-            const uint32_t k = maxima[i];
-            hi = max(hi, k);
-            if (k) lo = min(lo, k);
-        }
-        hi = __reduce_max_sync(0xffffffffu, hi);
-        lo = __reduce_min_sync(0xffffffffu, lo);
-        clear_bins(all);
-        if constexpr (kAll) {
-            if (lane == 0) {
-                sh.warp_hi[warp] = hi;
-                sh.warp_lo[warp] = lo;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                hi = max(hi, sh.warp_hi[w]);
-                lo = min(lo, sh.warp_lo[w]);
-            }
-        } else {
-            __syncwarp();
-        }
-        if (kAll ? tid == 0 : lane == 0) sh.kmax = hi;
-        int above = 0;
-        while (lo <= hi) {
-            const int shift = shift_of(hi - lo);
-            for (int i = t0; i < total; i += step) {
-                const uint32_t k = maxima[i];
-                if (k >= lo && k <= hi) atomicAdd(&sh.hist[top_slot(static_cast<int>((k - lo) >> shift))], 1);
-            }
-            team_sync(all);
-            if (!kAll || warp == 0) scan_bins(K - above, std::false_type());
-            team_sync(all);
-            const int bin = sh.bin, reach = sh.reach, past = sh.above;
-            if (bin < 0) break;  // fewer than K groups
-            T = lo + (static_cast<uint32_t>(bin) << shift);
-            if (above + reach <= K + K / 8 + 4 || shift == 0) break;
-            above += past;
-            lo = T;
-            hi = min(hi, T + ((1u << shift) - 1u));
-            clear_bins(all);
-            team_sync(all);
-        }
-        return max(T, kKeyNegInf);
-    };
-    uint32_t T;
-    if (total <= 512) {
-        __syncthreads();
-        if (warp == 0) {
-            T = find_theta(std::false_type());
-            if (lane == 0) sh.T = T;
-        }
-        __syncthreads();
-        T = sh.T;
-    } else {
-        T = find_theta(std::true_type());
-    }
-    const float theta = value_of(T);
-
-    // ---- sweep 2: the sum below theta and the candidates.  Each warp lists the chunks with an entry from theta
-    // on as it meets them and takes their entries afterwards, one a lane: the sum depends on no order
-    // but that of the row
-    // (exponents x c - M as one FMA, M = rn(theta c): one rounding, after the cancellation, and M belongs to the
-    // sum.  They stay below 1: x < theta)
-    const float c = p.c, M = theta == kNegInf ? 0.f : __fmul_rn(theta, c);
-    float S = 0.f;
-    bool over = false;
-    auto append = [&](float v, int j) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < p.room)
-            cand[at] = (static_cast<unsigned long long>(key_of(v)) << 32) | (0xffffffffu - static_cast<uint32_t>(j));
-    };
-    // whether a chunk has an entry from theta on (bf16: packed, theta rounded up to the entries' grid)
-    const uint32_t theta2 = __byte_perm(__float_as_uint(theta < 0.f ? theta : __uint_as_float((__float_as_uint(theta) + 0xffffu) & 0xffff0000u)), 0u, 0x3232);
-    auto reaches = [&](const uint4& r) {
-        if constexpr (sizeof(In) == 2) {
-            const uint32_t m = bmax2(bmax2(r.x, r.y), bmax2(r.z, r.w));
-            return any_ge2(m, theta2);
-        } else {
-            return E::max_raw(r) >= theta;
-        }
-    };
-    {
-        float2 acc = f2(0.f);
-        int hits = 0;
-        auto chunk = [&](const uint4& raw, int v, auto whole) {
-            const bool in = decltype(whole)::value || v < c1, hit = in && reaches(raw);
-            if constexpr (kRest) {
-                float y[kW];
-                E::unpack(raw, y);
-                float2 d[kW / 2];
-#pragma unroll
-                for (int e = 0; e < kW / 2; ++e) {
-                    const float2 a = fma2(make_float2(y[2 * e], y[2 * e + 1]), f2(c), f2(-M));
-                    d[e] = make_float2(ex2(a.x), ex2(a.y));
-                }
-#pragma unroll
-                for (int w = kW / 4; w > 0; w /= 2)
-#pragma unroll
-                    for (int e = 0; e < w; ++e) d[e] = add2(d[e], d[e + w]);
-                if (in && !hit) acc = add2(acc, d[0]);
-            }
-            const unsigned m = __ballot_sync(0xffffffffu, hit);
-            if (m) {
-                const int at = hits + __popc(m & ((1u << lane) - 1u));
-                if (hit && at < list_room) list[at] = static_cast<uint32_t>(v);
-                hits += __popc(m);
-            }
-        };
-        int v0 = c0 + warp * 32;
-        for (; v0 + 3 * kT + 32 <= c1; v0 += 4 * kT) {  // (four loads in flight)
-            uint4 raw[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) raw[i] = ldg_stream(body + size_t(v0 + i * kT + lane) * kW);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) chunk(raw[i], v0 + i * kT + lane, std::true_type());
-        }
-        if (v0 < c1) {
-            uint4 raw[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) raw[i] = ldg_stream(body + size_t(min(v0 + i * kT + lane, c1 - 1)) * kW);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (v0 + i * kT < c1) chunk(raw[i], v0 + i * kT + lane, std::false_type());
-        }
-        __syncwarp();
-        over |= hits > list_room;
-        hits = min(hits, list_room);
-        S += acc.x + acc.y;
-        // a listed chunk a lane, then, in the first warp, the single entries
-        for (int i = lane; i < hits; i += 32) {
-            const int v = static_cast<int>(list[i]);
-            float y[kW];
-            E::unpack(ldg_stream(body + size_t(v) * kW), y);
-#pragma unroll
-            for (int e = 0; e < kW; ++e) {
-                if (y[e] >= theta) append(y[e], v * kW + e - ph);
-                else if (kRest) S += ex2(fmaf(y[e], c, -M));
-            }
-        }
-        if (warp == 0 && lane < singles) {
-            const int j = single(lane);
-            const float v = E::load(x + j);
-            if (v >= theta) append(v, j);
-            else if (kRest) S += ex2(fmaf(v, c, -M));
-        }
-    }
-    if constexpr (kRest) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
-    }
-    if (lane == 0) {
-        sh.warp_f[warp] = S;
-        if (over) atomicAdd(&sh.n, 1 << 24);  // (above any room)
-    }
-    __syncthreads();
-    int n = sh.n, before = 0;
-    bool slow = n > p.room;
-    S = sh.warp_f[0];
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) S += sh.warp_f[w];
     const TopPart* parts;
     if (csize > 1) {
-        parts = exchange(TopPart{min(n, 1 << 24), slow ? 1 : 0, S, 0.f});
+        parts = exchange(TopPart{n, 0, S, 0.f});
         n = 0;
         S = 0.f;
         for (int r = 0; r < csize; ++r) {
             before += r < rank ? parts[r].n : 0;
             n += parts[r].n;
             S += parts[r].s;
-            slow |= parts[r].m != 0;
         }
+        slow = n > p.room;
     }
-    slow |= n > p.room;
-    float log_ref = mul_c(M, kLn2, kLn2Lo);  // the logarithm of what the sum is against
+    float log_ref = mul_c(Mt, kLn2, kLn2Lo);  // the logarithm of what the sum is against
     // the sum of the entries' exponentials below `bound` over the cluster, against the largest of them, m
     auto below = [&](float bound, float& m) {
         float mx = kNegInf;
@@ -492,27 +452,42 @@ __global__ void __launch_bounds__(kT, TOPK_R / kT) topk_kernel(TopParams p) {
         return sum;
     };
     if (slow) {
-        // the exact K-th largest key: theta itself if fewer than K entries lie above it
         auto block_sum = [&](int v) { return block_reduce<kT>(v, [](int a, int b) { return a + b; }, sh.warp_i); };
-        auto count = [&](auto pred) {
-            int m = 0;
-#pragma unroll 8
-            for (int j = first + tid; j < end; j += kT) m += pred(key_of(E::load(x + j))) ? 1 : 0;
-            m = block_sum(m);
-            const TopPart* q = exchange(TopPart{m, 0, 0.f, 0.f});
-            m = 0;
-            for (int r = 0; r < csize; ++r) m += q[r].n;
-            return m;
-        };
-        uint32_t kth = T;
-        if (sizeof(In) == 2 && !(T & 0x80000000u)) kth |= 0xffffu;  // (negative bf16 keys end in ones)
-        const uint32_t least = kth;
-        if (count([least](uint32_t k) { return k > least; }) >= K) {
-            kth = 0u;
-            for (int bit = 31; bit >= 0; --bit) {
-                const uint32_t at = kth | (1u << bit);
-                if (count([at](uint32_t k) { return k >= at; }) >= K) kth = at;
+        // the exact K-th largest key: histograms of all keys, refined in its bin down to one key.  (At least K
+        // entries are theta or larger, or theta is -inf.)
+        uint32_t lo = T, hi = kmax, kth = T;
+        for (int need = K; lo <= hi;) {
+            const int shift = shift_of(hi - lo);
+            for (int i = tid; i < kTopBins; i += kT) sh.hist[i] = 0;
+            if (csize > 1) {
+                cluster_arrive_release();
+                cluster_wait();
+            } else {
+                __syncthreads();
             }
+#pragma unroll 4
+            for (int j = first + tid; j < end; j += kT) {
+                const uint32_t k = key_of(E::load(x + j));
+                if (k >= lo && k <= hi) atomicAdd(&sh.hist[(k - lo) >> shift], 1);
+            }
+            __syncthreads();
+            if (rank > 0)
+                for (int i = tid; i < kTopBins; i += kT)
+                    if (sh.hist[i]) add_dsmem_s32(map_rank(&sh.hist[i], 0u), sh.hist[i]);
+            if (csize > 1) {
+                cluster_arrive_release();
+                cluster_wait();
+            }
+            if (warp == 0) scan_bins(need, std::false_type());
+            __syncthreads();
+            const TopPart* q = exchange(TopPart{sh.bin, sh.above, 0.f, 0.f});
+            const int bin = q[0].n, past = q[0].m;  // of the first CTA, which has all counts
+            if (bin < 0) break;                     // fewer than K numbers
+            kth = lo + (static_cast<uint32_t>(bin) << shift);
+            if (shift == 0) break;
+            need -= past;
+            lo = kth;
+            hi = min(hi, kth + ((1u << shift) - 1u));
         }
         T = kth;
         // the entries above it, then those equal to it, in index order: warps own runs of entries
@@ -590,39 +565,67 @@ __global__ void __launch_bounds__(kT, TOPK_R / kT) topk_kernel(TopParams p) {
         if (rank > 0) return;
         cluster_wait();
     }
-    // By the bin of each candidate's value; those of one bin compare with each other.  T and the largest maximum
-    // bound the values, but for NaN, which goes to the last bin.
-    const uint32_t range = sh.kmax > T ? sh.kmax - T : 0u;
-    const int shift = shift_of(range);
-    auto bin_of = [&](unsigned long long k) {
-        const uint32_t v = static_cast<uint32_t>(k >> 32);
-        return top_slot(static_cast<int>(min(v > T ? v - T : 0u, range) >> shift));
+    auto emit = [&](unsigned long long k, int r) {
+        if (r < K) {
+            values[r] = cand_value(k);
+            ids[r] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(k));
+        } else if (r == K) {
+            sh.ref = cand_value(k);
+        }
     };
-    unsigned short* place = reinterpret_cast<unsigned short*>(lists);
-    auto finish = [&](auto all) {
-        constexpr bool kAll = decltype(all)::value;
-        const int t0 = kAll ? tid : lane, step = kAll ? kT : 32;
-        auto emit = [&](unsigned long long k, int r) {
-            if (r < K) {
-                values[r] = value_of(static_cast<uint32_t>(k >> 32));
-                ids[r] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(k));
-            } else if (r == K) {
-                sh.ref = value_of(static_cast<uint32_t>(k >> 32));
+    // the candidates that were not taken, against the largest of them
+    unsigned long long left = 0ull;
+    auto leave = [&](unsigned long long k) { left += __float2ull_rn(ex2((cand_value(k) - sh.ref) * c) * kTopFix); };
+    if (n <= kTopCountMost) {
+        constexpr int kMost = (kTopCountMost + kT - 1) / kT;
+        unsigned long long k[kMost];
+        int r[kMost];
+#pragma unroll
+        for (int u = 0; u < kMost; ++u) {
+            const int i = tid + u * kT;
+            k[u] = i < n ? cand[i] : 0ull;
+            r[u] = 0;
+            if (i - lane < n) {
+                int j = 0;
+                for (; j + 8 <= n; j += 8) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(cand + j + e);
+                        r[u] += (o.x > k[u] ? 1 : 0) + (o.y > k[u] ? 1 : 0);
+                    }
+                }
+                for (; j < n; ++j) r[u] += cand[j] > k[u] ? 1 : 0;
+                if (i < n) emit(k[u], r[u]);
             }
+        }
+        if (kRest && n > K) {
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < kMost; ++u)
+                if (tid + u * kT < n && r[u] >= K) leave(k[u]);
+        }
+    } else {
+        // By the bin of each candidate's value; those of one bin compare with each other.  T and the largest
+        // maximum bound the values, but for NaN, which goes to the last bin.
+        const uint32_t range = kmax > T ? kmax - T : 0u;
+        const int shift = shift_of(range);
+        auto bin_of = [&](unsigned long long k) {
+            const uint32_t v = static_cast<uint32_t>(k >> 32);
+            return static_cast<int>(min(v > T ? v - T : 0u, range) >> shift);
         };
-        clear_bins(all);
-        team_sync(all);
-        for (int i = t0; i < n; i += step)
+        for (int i = tid; i < kTopBins; i += kT) sh.hist[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += kT)
             place[i] = static_cast<unsigned short>(atomicAdd(&sh.hist[bin_of(cand[i])], 1));  // in its bin
-        team_sync(all);
-        if (!kAll || warp == 0) scan_bins(K, std::true_type());
-        team_sync(all);
+        __syncthreads();
+        if (warp == 0) scan_bins(K, std::true_type());
+        __syncthreads();
         if (sh.crowd <= kTopCrowd) {
-            for (int i = t0; i < n; i += step) sorted[sh.base[bin_of(cand[i])] + place[i]] = cand[i];
-            team_sync(all);
-            for (int i = t0; i < n; i += step) {
+            for (int i = tid; i < n; i += kT) sorted[sh.base[bin_of(cand[i])] + place[i]] = cand[i];
+            __syncthreads();
+            for (int i = tid; i < n; i += kT) {
                 const unsigned long long k = sorted[i];
-                const int slot = bin_of(k), from = sh.base[slot], to = from + sh.hist[slot];
+                const int bin = bin_of(k), from = sh.base[bin], to = from + sh.hist[bin];
                 int at = from;
                 for (int j = from; j < to; ++j) at += sorted[j] > k ? 1 : 0;
                 emit(k, at);
@@ -631,11 +634,11 @@ __global__ void __launch_bounds__(kT, TOPK_R / kT) topk_kernel(TopParams p) {
         } else {  // many equal values: a bitonic sort
             int size = 1;
             while (size < n) size <<= 1;  // <= room
-            for (int i = t0; i < size; i += step) sorted[i] = i < n ? cand[i] : 0ull;
+            for (int i = tid; i < size; i += kT) sorted[i] = i < n ? cand[i] : 0ull;
             for (int k = 2; k <= size; k <<= 1) {
                 for (int j = k >> 1; j > 0; j >>= 1) {
-                    team_sync(all);
-                    for (int t = t0; t < size / 2; t += step) {
+                    __syncthreads();
+                    for (int t = tid; t < size / 2; t += kT) {
                         const int a = 2 * t - (t & (j - 1)), b = a + j;
                         const unsigned long long va = sorted[a], vb = sorted[b];
                         const bool descending = (a & k) == 0;
@@ -646,58 +649,50 @@ __global__ void __launch_bounds__(kT, TOPK_R / kT) topk_kernel(TopParams p) {
                     }
                 }
             }
-            team_sync(all);
-            for (int i = t0; i < n; i += step) {
+            __syncthreads();
+            for (int i = tid; i < n; i += kT) {
                 emit(sorted[i], i);
                 place[i] = static_cast<unsigned short>(i);
             }
         }
-        for (int i = n + t0; i < K; i += step) {  // fewer than K numbers in the row
-            values[i] = kNegInf;
-            ids[i] = -1;
+        if (kRest && n > K) {
+            __syncthreads();
+            for (int i = tid; i < n; i += kT)
+                if (place[i] >= K) leave(sorted[i]);
         }
-        if constexpr (kRest) {
-            if (n > K) {  // the candidates that were not taken, against the largest of them
-                team_sync(all);
+    }
+    for (int i = n + tid; i < K; i += kT) {  // fewer than K numbers in the row
+        values[i] = kNegInf;
+        ids[i] = -1;
+    }
+    if constexpr (kRest) {
+        if (n > K) {
+            if (__any_sync(0xffffffffu, left != 0ull)) {
+                left = warp_sum_u64(left);
+                if (lane == 0) atomicAdd(&sh.left, left);
+            }
+            __syncthreads();
+            if (tid == 0) {
                 const float v = sh.ref;
-                unsigned long long left = 0ull;
-                for (int i = t0; i < n; i += step)
-                    if (place[i] >= K)
-                        left += __float2ull_rn(ex2((value_of(static_cast<uint32_t>(sorted[i] >> 32)) - v) * c) * kTopFix);
-                if (__any_sync(0xffffffffu, left != 0ull)) {
-                    left = warp_sum_u64(left);
-                    if (kAll && lane == 0) atomicAdd(&sh.left, left);
-                }
-                if constexpr (kAll) {
-                    __syncthreads();
-                    left = sh.left;
-                }
-                S = (S > 0.f ? S * ex2(fmaf(-v, c, M)) : 0.f) + __ull2float_rn(left) * (1.f / kTopFix);
+                S = (S > 0.f ? S * ex2(fmaf(-v, c, Mt)) : 0.f) + __ull2float_rn(sh.left) * (1.f / kTopFix);
                 log_ref = __fdiv_rn(v, p.tau);
             }
-            if (t0 == 0) p.rest[row] = S > 0.f ? fmaf(log2f(S), kLn2, log_ref) : kNegInf;
         }
-    };
-    if (n <= 128) {
-        __syncthreads();
-        if (warp == 0) finish(std::false_type());
-    } else {
-        finish(std::true_type());
+        if (tid == 0) p.rest[row] = S > 0.f ? fmaf(log2f(S), kLn2, log_ref) : kNegInf;
     }
 }
 
 template <typename In, int kT>
 static osd_status launch_topk(TopParams tp, long long rows, int c, cudaStream_t s) {
-    constexpr int kW = Elem<In>::kVec;
-    const int positions = tp.V + kW - 1;  // a row starts up to kW - 1 positions into the grid
+    const int positions = tp.V + Elem<In>::kVec - 1;  // a row starts up to kVec - 1 positions into the grid
     c = std::max(1, std::min(c, kTopMaxCluster));
     tp.span = ((positions + c - 1) / c + 63) / 64 * 64;
     tp.csize = (positions + tp.span - 1) / tp.span;
     tp.room = 256;
     while (tp.room < tp.K + tp.K / 2 + 128) tp.room *= 2;
-    const int per = (tp.span / kW + kT - 1) / kT;  // chunks per thread
-    tp.groups = std::max(1, std::min(per, (4 * tp.K + tp.csize * kT - 1) / (tp.csize * kT)));
-    const size_t smem = size_t(tp.room) * 24 + size_t(tp.csize) * kT * tp.groups * 4;
+    tp.maxima = 1;
+    while (tp.maxima < kTopGroups && tp.csize * kT * tp.maxima < 4 * tp.K) tp.maxima *= 2;
+    const size_t smem = size_t(tp.room) * 18 + size_t(tp.csize) * kT * tp.maxima * 4 + size_t(kT) * kTopGroups;
     if (rows * tp.csize > INT_MAX) return OSD_ERR_UNSUPPORTED;
     auto go = [&](auto kernel_tag) -> osd_status {
         constexpr bool kRest = decltype(kernel_tag)::value;
@@ -710,9 +705,15 @@ static osd_status launch_topk(TopParams tp, long long rows, int c, cudaStream_t 
 
 template <typename In>
 static osd_status launch_topk_dtype(const TopParams& tp, long long rows, cudaStream_t s) {
-    const long long bytes = (long long)tp.V * (long long)sizeof(In);
-    const int c = TOPK_C(bytes, rows);
-    switch (TOPK_T) {
+    const int chunks = static_cast<int>((tp.V + Elem<In>::kVec - 1) / Elem<In>::kVec);
+    // about 16 to 64 chunks a thread; calls that leave SMs idle take more threads a row, while each has 4
+    // chunks or more, and then more CTAs.  (@@)
+    const long long slots = (long long)device_sms() * 1024;
+    int t = chunks <= 1024 ? 64 : (chunks <= 8192 ? 128 : (chunks <= 24576 ? 256 : 512)), c = 1;
+    while (t < 512 && rows * 2 * t <= slots && chunks >= 8 * t) t *= 2;
+    while (c < kTopMaxCluster && rows * 2 * t * c <= slots && chunks > 12 * t * c) c *= 2;
+    switch (t) {
+        case 64: return launch_topk<In, 64>(tp, rows, c, s);
         case 128: return launch_topk<In, 128>(tp, rows, c, s);
         case 256: return launch_topk<In, 256>(tp, rows, c, s);
         default: return launch_topk<In, 512>(tp, rows, c, s);
