@@ -126,8 +126,8 @@ template <> struct ChunkMax<__nv_bfloat16> {
     __device__ __forceinline__ float top() const { return fmaxf(bf16_lo(m), bf16_hi(m)); }
 };
 
-template <typename In, bool kRest, int kT>
-__global__ void __launch_bounds__(kT, 1024 / kT) topk_kernel(TopParams p) {
+template <typename In, bool kRest, int kT, bool kFew>
+__global__ void __launch_bounds__(kT, kFew ? 1 : (kT == 128 ? 1280 : 1024) / kT) topk_kernel(TopParams p) {
     using E = Elem<In>;
     constexpr int kW = E::kVec, kWarps = kT / 32, kG = kTopGroups;
     extern __shared__ __align__(128) unsigned char dsm[];
@@ -160,7 +160,11 @@ __global__ void __launch_bounds__(kT, 1024 / kT) topk_kernel(TopParams p) {
     unsigned long long* cand = reinterpret_cast<unsigned long long*>(dsm);
     unsigned long long* sorted = cand + p.room;
     uint32_t* maxima = reinterpret_cast<uint32_t*>(sorted + p.room);
-    unsigned short* place = reinterpret_cast<unsigned short*>(maxima + csize * kT * p.maxima);
+    // per warp: its groups, and its chunks, with an entry from theta on
+    const int chunk_room = 2 * p.room / kWarps;
+    uint32_t* chunk_lists = maxima + csize * kT * p.maxima;
+    uint32_t* chunk_list = chunk_lists + warp * chunk_room;
+    unsigned short* place = reinterpret_cast<unsigned short*>(chunk_lists + 2 * p.room);
     unsigned char* list = reinterpret_cast<unsigned char*>(place + p.room) + warp * (32 * kG);
     if (tid == 0) {
         sh.n = 0;
@@ -191,7 +195,7 @@ __global__ void __launch_bounds__(kT, 1024 / kT) topk_kernel(TopParams p) {
         return d[0].x + d[0].y;
     };
     const int v0 = c0 + tid;
-    constexpr int kHalf = kG / 2;
+    constexpr int kHalf = kFew ? kG : kG / 2;  // loads in flight
     for (int v = v0; v < c1; v += kG * kT) {
 #pragma unroll
         for (int h = 0; h < kG; h += kHalf) {
@@ -346,6 +350,7 @@ __global__ void __launch_bounds__(kT, 1024 / kT) topk_kernel(TopParams p) {
     // too.  A warp lists its groups in one order, so that the sum depends on none.
     const float Mt = theta == kNegInf ? 0.f : __fmul_rn(theta, c);
     float S = 0.f;
+    bool over = false;
     auto append = [&](float v, int j) {
         const int at = atomicAdd(&sh.n, 1);
         if (at < p.room) cand[at] = cand_of(v, j);
@@ -363,21 +368,60 @@ __global__ void __launch_bounds__(kT, 1024 / kT) topk_kernel(TopParams p) {
             hits += __popc(m);
         }
         __syncwarp();
+        // the chunks of these groups, a group a lane: those below theta join the sum, the others a second list
+        // (where a group is one chunk, the list is that of the groups)
+        const bool lone = c1 - c0 <= kG * kT;
+        int chunks = lone ? hits : 0;
+        for (int i0 = 0; i0 < hits && !lone; i0 += 32) {
+            const int at = i0 + lane < hits ? list[i0 + lane] : -1;
+            const int w0 = c0 + warp * 32 + at / kG + (at % kG) * kT;
+            for (int b = c0; b < c1; b += 4 * kG * kT) {
+                uint4 raw[4];
+                bool in[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int v = w0 + (b - c0) + u * (kG * kT);
+                    in[u] = at >= 0 && v < c1;
+                    raw[u] = ninf_raw<In>();
+                    if (in[u]) raw[u] = ldg_nc(body + size_t(v) * kW);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (b + u * (kG * kT) >= c1) break;
+                    const bool is = in[u] && E::max_raw(raw[u]) >= theta;
+                    if constexpr (kRest) {
+                        const float e = exps(raw[u], Mt);
+                        if (in[u] && !is) S += e;
+                    }
+                    const unsigned m = __ballot_sync(0xffffffffu, is);
+                    if (is) {
+                        const int to = chunks + __popc(m & ((1u << lane) - 1u));
+                        if (to < chunk_room) chunk_list[to] = static_cast<uint32_t>(w0 + (b - c0) + u * (kG * kT));
+                    }
+                    chunks += __popc(m);
+                }
+            }
+        }
+        if (!lone) {
+            over = chunks > chunk_room;
+            chunks = min(chunks, chunk_room);
+        }
+        __syncwarp();
+        // and their entries, a chunk a lane, with those outside whole chunks
         auto entry = [&](float y, int j) {
             if (y >= theta) append(y, j);
             else if (kRest) S += ex2(fmaf(y, c, -Mt));
         };
-        for (int i = lane; i < hits; i += 32) {
-            const int at = list[i];
-            for (int v = c0 + warp * 32 + at / kG + (at % kG) * kT; v < c1; v += kG * kT) {
-                float y[kW];
-                E::unpack(load(v), y);
+        for (int i = lane; i < chunks; i += 32) {
+            const int v = lone ? c0 + warp * 32 + list[i] / kG + (list[i] % kG) * kT : static_cast<int>(chunk_list[i]);
+            float y[kW];
+            E::unpack(ldg_nc(body + size_t(v) * kW), y);
 #pragma unroll
-                for (int e = 0; e < kW; ++e) entry(y[e], v * kW + e - ph);
-            }
+            for (int e = 0; e < kW; ++e) entry(y[e], v * kW + e - ph);
         }
         if (tid < singles) entry(E::load(x + single(tid)), single(tid));
     }
+    if (over && lane == 0) atomicAdd(&sh.n, 1 << 24);  // (above any room)
     if constexpr (kRest) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
@@ -414,7 +458,7 @@ __global__ void __launch_bounds__(kT, 1024 / kT) topk_kernel(TopParams p) {
     };
     const TopPart* parts;
     if (csize > 1) {
-        parts = exchange(TopPart{n, 0, S, 0.f});
+        parts = exchange(TopPart{min(n, 1 << 24), 0, S, 0.f});
         n = 0;
         S = 0.f;
         for (int r = 0; r < csize; ++r) {
@@ -682,7 +726,7 @@ __global__ void __launch_bounds__(kT, 1024 / kT) topk_kernel(TopParams p) {
     }
 }
 
-template <typename In, int kT>
+template <typename In, int kT, bool kFew>
 static osd_status launch_topk(TopParams tp, long long rows, int c, cudaStream_t s) {
     const int positions = tp.V + Elem<In>::kVec - 1;  // a row starts up to kVec - 1 positions into the grid
     c = std::max(1, std::min(c, kTopMaxCluster));
@@ -692,12 +736,12 @@ static osd_status launch_topk(TopParams tp, long long rows, int c, cudaStream_t 
     while (tp.room < tp.K + tp.K / 2 + 128) tp.room *= 2;
     tp.maxima = 1;
     while (tp.maxima < kTopGroups && tp.csize * kT * tp.maxima < 4 * tp.K) tp.maxima *= 2;
-    const size_t smem = size_t(tp.room) * 18 + size_t(tp.csize) * kT * tp.maxima * 4 + size_t(kT) * kTopGroups;
+    const size_t smem = size_t(tp.room) * 26 + size_t(tp.csize) * kT * tp.maxima * 4 + size_t(kT) * kTopGroups;
     if (rows * tp.csize > INT_MAX) return OSD_ERR_UNSUPPORTED;
     auto go = [&](auto kernel_tag) -> osd_status {
         constexpr bool kRest = decltype(kernel_tag)::value;
-        if (ctas_per_sm<topk_kernel<In, kRest, kT>, kT>(smem) < 1) return OSD_ERR_CUDA;  // (opts in for the size)
-        return from_cuda(launch_ex(true, topk_kernel<In, kRest, kT>, dim3(static_cast<unsigned>(rows * tp.csize)), dim3(kT),
+        if (ctas_per_sm<topk_kernel<In, kRest, kT, kFew>, kT>(smem) < 1) return OSD_ERR_CUDA;  // (opts in for the size)
+        return from_cuda(launch_ex(true, topk_kernel<In, kRest, kT, kFew>, dim3(static_cast<unsigned>(rows * tp.csize)), dim3(kT),
                                    smem, s, tp.csize, tp));
     };
     return tp.rest ? go(std::true_type()) : go(std::false_type());
@@ -710,13 +754,14 @@ static osd_status launch_topk_dtype(const TopParams& tp, long long rows, cudaStr
     // chunks or more, and then more CTAs.  (@@)
     const long long slots = (long long)device_sms() * 1024;
     int t = chunks <= 1024 ? 64 : (chunks <= 8192 ? 128 : (chunks <= 24576 ? 256 : 512)), c = 1;
-    while (t < 512 && rows * 2 * t <= slots && chunks >= 8 * t) t *= 2;
+    while (t < 512 && (rows * 2 * t <= slots || t < tp.K) && chunks >= 8 * t) t *= 2;
     while (c < kTopMaxCluster && rows * 2 * t * c <= slots && chunks > 12 * t * c) c *= 2;
+    if (t == 512 && rows * c <= device_sms() * (tp.mask ? 2 : 1)) return launch_topk<In, 512, true>(tp, rows, c, s);
     switch (t) {
-        case 64: return launch_topk<In, 64>(tp, rows, c, s);
-        case 128: return launch_topk<In, 128>(tp, rows, c, s);
-        case 256: return launch_topk<In, 256>(tp, rows, c, s);
-        default: return launch_topk<In, 512>(tp, rows, c, s);
+        case 64: return launch_topk<In, 64, false>(tp, rows, c, s);
+        case 128: return launch_topk<In, 128, false>(tp, rows, c, s);
+        case 256: return launch_topk<In, 256, false>(tp, rows, c, s);
+        default: return launch_topk<In, 512, false>(tp, rows, c, s);
     }
 }
 
