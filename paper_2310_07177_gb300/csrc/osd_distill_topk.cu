@@ -10,9 +10,17 @@
 // one factor for all the other tokens and one value for each kept token.  So a row
 // needs the sum of its other entries' exponentials (summed on its own: 1 - sum of the kept
 // ones would cancel), K + 1 classes' worth of arithmetic, and one scaled exponential an entry.
+//
+// One thread-block cluster per row, each CTA with a span of it in shared memory (one bulk
+// copy).  While that flies, the CTA takes the kept tokens: the target's distribution, and the
+// draft's logits there, gathered from global memory so that every CTA has them all.  Then the kept
+// entries are set to -inf in the staged span; its sum of exponentials meets the others by st.async; the classes
+// follow, by every CTA alike; and a second sweep over the span writes the gradient.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "osd.h"
 #include "osd_device.cuh"
@@ -20,8 +28,17 @@
 
 namespace osd {
 
-constexpr int kDtThreads = 256;
+#ifndef DT_SPAN
+#define DT_SPAN 32768
+#define DT_R 1280
+#endif
+constexpr int kDtThreads = 128;
+constexpr int kDtWarps = kDtThreads / 32;
+constexpr int kDtMaxCluster = 8;
 constexpr int kDtMaxV = 393216;
+constexpr uint64_t kDtStageWaitNs = 1000000000ull;  // bound on the wait for the bulk copy ...
+constexpr uint64_t kDtPeerWaitNs = 3000000000ull;   // ... and for the peers' sums
+constexpr float kDtRefMax = 4294967296.f;           // a warp's sum past this takes its true maximum
 
 struct DtParams {
     const void* draft;
@@ -39,6 +56,8 @@ struct DtParams {
     float* loss;
     float* dlogits;
     int32_t* status;
+    int csize;  // CTAs per row
+    int span;   // positions per CTA, whole chunks
 };
 
 // log2 of exp(rest) against exp(v / tau), rest and v / tau of any size: each product keeps
@@ -87,110 +106,264 @@ __device__ __forceinline__ float class_factor(float p, float lp, float q, float 
     return q > p ? s.z + 0.5f * eq : (q < p ? -(s.y + 0.5f * eq) : 0.5f * (s.z - s.y));
 }
 
+// What every CTA derives from the cluster's sums.
+struct DtSums {
+    float M, S;     // the others: sum of 2^(x c - M)
+    float lgZ, inv_Z;  // the normaliser against the largest exponent of all ...
+    float dz, w;    // ... that of the largest kept logit, and the probability of an other token per 2^(x c - M)
+    float pr, lpr, qr, lqr;
+    float coef;     // FKL, CE: of the others' gradient
+    int bad;
+};
+
+// 2^(a - b), 0 for a = -inf
+__device__ __forceinline__ float dt_to_ref(float a, float b) { return a == kNegInf ? 0.f : ex2(a - b); }
+
 template <typename In, int kKind>
-__global__ void __launch_bounds__(kDtThreads) distill_topk_kernel(DtParams p) {
+__global__ void __launch_bounds__(kDtThreads, DT_R / kDtThreads) distill_topk_kernel(DtParams p) {
     using E = Elem<In>;
-    extern __shared__ uint32_t s_bits[];  // which entries are kept
-    __shared__ float s_v[OSD_TOPK_MAX_K], s_z[OSD_TOPK_MAX_K];
-    __shared__ int s_id[OSD_TOPK_MAX_K];
+    constexpr int kW = E::kVec, kT = kDtThreads;
+    extern __shared__ __align__(128) unsigned char dsm[];
+    __shared__ __align__(16) float4 s_recv[kDtMaxCluster];  // slot r from CTA r
+    __shared__ __align__(8) uint64_t s_bar, s_peer;
+    __shared__ float2 s_part[kDtWarps];
+    __shared__ float3 s_terms[kDtWarps];
+    __shared__ MaxIdx s_best[kDtWarps];
+    __shared__ float s_wz[kDtWarps], s_wl[kDtWarps], s_we[kDtWarps];
+    __shared__ DtSums sm;
     __shared__ int s_bad;
-    __shared__ float s_red[kDtThreads / 32];
-    __shared__ float3 s_red3[kDtThreads / 32];
-    __shared__ MaxIdx s_redi[kDtThreads / 32];
-    const int tid = threadIdx.x;
-    const long long row = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int csize = p.csize, rank = csize > 1 ? static_cast<int>(cluster_rank()) : 0;
+    const unsigned row = csize > 1 ? blockIdx.x / static_cast<unsigned>(csize) : blockIdx.x;
     const int V = p.V, K = p.K;
     grid_dependency_sync();
-    if (p.mask && !p.mask[row]) {
-        if (tid == 0) p.loss[row] = 0.f;
+    if (p.mask && !p.mask[row]) {  // the cluster alike
+        if (rank == 0 && tid == 0) p.loss[row] = 0.f;
         return;
     }
-    const In* x = static_cast<const In*>(p.draft) + (row / p.P) * p.dsg + (row % p.P) * p.dsp;
-    float* out = p.dlogits + row * V;
-    auto add = [](float a, float b) { return a + b; };
-    auto most = [](float a, float b) { return fmaxf(a, b); };
-    if (tid == 0) s_bad = 0;
-    for (int i = tid; i < (V + 31) / 32; i += kDtThreads) s_bits[i] = 0u;
+    unsigned group = row, pos = 0;
+    if (p.P > 1) {
+        group = row / static_cast<unsigned>(p.P);
+        pos = row - group * static_cast<unsigned>(p.P);
+    }
+    const In* x = static_cast<const In*>(p.draft) + group * p.dsg + pos * p.dsp;
+    float* out = p.dlogits + size_t(row) * V;
+    // entry j counts as position j + ph: chunks of positions are 16-byte vectors of the row
+    const int ph = static_cast<int>((reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(In));
+    const int p0 = rank * p.span, p1 = min(p0 + p.span, V + ph);  // this CTA's positions, in n chunks,
+    const int n = max(0, (p1 - p0 + kW - 1) / kW);
+    const int c0 = p0 < ph ? 1 : 0;                                  // of which [c0, c1) lie within the row
+    const int c1 = max(c0, p0 + n * kW > V + ph ? n - 1 : n);
+    In* staged = reinterpret_cast<In*>(dsm);
+    int* s_id = reinterpret_cast<int*>(dsm + size_t(p.span) * sizeof(In));
+    float* s_t = reinterpret_cast<float*>(s_id + K);  // log2 of the target's weight against the largest kept
+    float* s_e = s_t + K;                             // (z - zmax) c
+    uint32_t* s_seen = reinterpret_cast<uint32_t*>(s_e + K);  // which of this CTA's positions are kept
+    if (tid == 0) {
+        s_bad = 0;
+        mbar_init_only(&s_bar, 1);
+        mbar_init_only(&s_peer, 1);
+        fence_mbarrier_init();
+        if (c1 > c0) {
+            const uint32_t bytes = static_cast<uint32_t>(c1 - c0) * 16u;
+            mbar_arrive_expect_tx(&s_bar, bytes);
+            bulk_g2s(staged + c0 * kW, x + (p0 + c0 * kW - ph), bytes, &s_bar);
+        }
+    }
+    if (csize > 1) cluster_arrive_relaxed();  // peers may push once this CTA's barrier is there
+    for (int i = tid; i < (n * kW + 31) / 32; i += kT) s_seen[i] = 0u;
+    auto fringe = [&](int chunk) {  // a chunk that reaches past the row
+        if (tid < kW) {
+            const int j = p0 + chunk * kW + tid - ph;
+            E::store(staged + chunk * kW + tid, j >= 0 && j < V ? E::load(x + j) : kNegInf);
+        }
+    };
+    if (c0 == 1 && n > 0) fringe(0);
+    if (c1 < n && c1 >= c0) fringe(n - 1);
     __syncthreads();
-    MaxIdx best{kNegInf, INT_MAX};  // the largest value, with the lowest id
-    for (int i = tid; i < K; i += kDtThreads) {
-        const int id = p.ids[row * K + i];
-        const float v = p.values[row * K + i];
-        s_id[i] = id;
-        s_v[i] = v;
-        if (id < 0) continue;
-        if (id >= V) {
-            s_bad = 1;
-            continue;
-        }
-        if (atomicOr(&s_bits[id >> 5], 1u << (id & 31)) >> (id & 31) & 1u) s_bad = 1;
-        s_z[i] = E::load(x + id);
-        best = merge_mi(best, MaxIdx{v, id});
-    }
-    best = block_reduce<kDtThreads>(best, [](MaxIdx a, MaxIdx b) { return merge_mi(a, b); }, s_redi);
-    const bool bad = s_bad;
-    const float vref = best.m, rest = (p.rest && kKind != OSD_CE) ? p.rest[row] : kNegInf;
-    if (bad || fmaxf(vref, rest) == kNegInf) {  // a bad row, or no target mass
-        for (int j = tid; j < V; j += kDtThreads) out[j] = 0.f;
-        if (tid == 0) {
-            p.loss[row] = bad ? __int_as_float(0x7fc00000) : 0.f;
-            if (bad && p.status) atomicExch(p.status, static_cast<int32_t>(OSD_ERR_INVALID_ARG));
-        }
-        return;
-    }
-    // ---- the target: t_c = log2 of the class's weight against the largest kept value's
+
+    // ---- the kept tokens: the largest value with its lowest id, and the largest draft logit
     const float c = p.c, ch = p.c_hi, cl = p.c_lo;
+    MaxIdx best{kNegInf, INT_MAX};
+    float zmax = kNegInf;
+    for (int i = tid; i < K; i += kT) {
+        const int id = p.ids[size_t(row) * K + i];
+        float v = p.values[size_t(row) * K + i], z = kNegInf;
+        if (id >= V) s_bad = 1;
+        const bool used = id >= 0 && id < V;
+        if (used) {
+            z = E::load(x + id);
+            best = merge_mi(best, MaxIdx{v, id});
+            zmax = fmaxf(zmax, z);
+            const int at = id + ph - p0;
+            if (at >= 0 && at < p1 - p0 && (atomicOr(&s_seen[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u)) s_bad = 1;
+        } else {
+            v = kNegInf;
+        }
+        s_id[i] = used ? id : -1;
+        s_t[i] = v;
+        s_e[i] = z;
+    }
+    best = warp_reduce(best, [](MaxIdx a, MaxIdx b) { return merge_mi(a, b); });
+    zmax = warp_reduce(zmax, [](float a, float b) { return fmaxf(a, b); });
+    if (lane == 0) {
+        s_best[warp] = best;
+        s_wz[warp] = zmax;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kDtWarps; ++w) {
+        best = merge_mi(best, s_best[w]);
+        zmax = fmaxf(zmax, s_wz[w]);
+    }
+    const float vref = best.m, rest = (p.rest && kKind != OSD_CE) ? p.rest[row] : kNegInf;
+    const bool empty = fmaxf(vref, rest) == kNegInf;  // no target mass
+    // t_c: log2 of the class's weight against the largest kept value's; mt: their largest
     const float tr = rest == kNegInf ? kNegInf : (vref == kNegInf ? 0.f : rest_minus(rest, vref, ch, cl));
     const float mt = vref == kNegInf ? tr : fmaxf(0.f, tr);
-    auto t_of = [&](int i) { return (s_v[i] == kNegInf) ? kNegInf : mul_c(s_v[i] - vref, ch, cl) - mt; };
-    float L = 0.f;
-    for (int i = tid; i < K; i += kDtThreads)
-        if (s_id[i] >= 0) L += ex2(t_of(i));
-    L = block_reduce<kDtThreads>(L, add, s_red) + ex2(tr - mt);
+    float L = 0.f, Zc = 0.f;
+    for (int i = tid; i < K; i += kT) {
+        const float v = s_t[i], z = s_e[i];
+        const float t = v == kNegInf ? kNegInf : mul_c(v - vref, ch, cl) - mt, e = z == kNegInf ? kNegInf : mul_c(z - zmax, ch, cl);
+        s_t[i] = t;
+        s_e[i] = e;
+        L += ex2(t);
+        Zc += ex2(e);
+    }
+    L = warp_reduce(L, [](float a, float b) { return a + b; });
+    Zc = warp_reduce(Zc, [](float a, float b) { return a + b; });
+    if (lane == 0) {
+        s_wl[warp] = L;
+        s_we[warp] = Zc;
+    }
+    // ---- the staged span: kept entries leave it
+    bool late = false;
+    if (c1 > c0 && !mbar_wait_bounded(&s_bar, 0, kDtStageWaitNs)) {
+        late = true;
+        mbar_wait_bounded(&s_bar, 0, kDtStageWaitNs);  // give the copy in flight a last chance to land
+    }
+    for (int i = tid; i < K; i += kT) {
+        const int at = s_id[i] + ph - p0;
+        if (s_id[i] >= 0 && at >= 0 && at < p1 - p0) E::store(staged + at, kNegInf);
+    }
+    const bool failed = __syncthreads_or(late);
+    L = ex2(tr - mt);
+    Zc = 0.f;
+#pragma unroll
+    for (int w = 0; w < kDtWarps; ++w) {
+        L += s_wl[w];
+        Zc += s_we[w];
+    }
+    // ---- the others' exponentials against the warp's reference, the largest entry of its first chunks: sums past
+    // 2^32, and warps whose first chunks hold nothing, take the true maximum first
+    const float2 mine = [&]() {
+        float m = kNegInf;
+        if (tid < n) m = E::max_raw(lds_v4(staged + tid * kW));
+        float M, s;
+        for (int pass = 0;; ++pass) {
+            m = warp_reduce(m, [](float a, float b) { return fmaxf(a, b); });
+            M = m == kNegInf ? 0.f : __fmul_rn(m, c);
+            float2 acc = f2(0.f);
+#pragma unroll 2
+            for (int v = tid; v < n; v += kT) {
+                float y[kW];
+                E::unpack(lds_v4(staged + v * kW), y);
+                float2 d[kW / 2];
+#pragma unroll
+                for (int e = 0; e < kW / 2; ++e) {
+                    const float2 a = fma2(make_float2(y[2 * e], y[2 * e + 1]), f2(c), f2(-M));
+                    d[e] = make_float2(ex2(a.x), ex2(a.y));
+                }
+#pragma unroll
+                for (int w = kW / 4; w > 0; w /= 2)
+#pragma unroll
+                    for (int e = 0; e < w; ++e) d[e] = add2(d[e], d[e + w]);
+                acc = add2(acc, d[0]);
+            }
+            s = warp_reduce(acc.x + acc.y, [](float a, float b) { return a + b; });
+            if (pass == 1 || (m != kNegInf && s < kDtRefMax)) break;
+            m = kNegInf;
+            for (int v = tid; v < n; v += kT) m = fmaxf(m, E::max_raw(lds_v4(staged + v * kW)));
+        }
+        return make_float2(m == kNegInf ? kNegInf : M, s);
+    }();
+    if (lane == 0) s_part[warp] = mine;
+    __syncthreads();
+    // ---- the cluster's sum, and what follows from it, by warp 0 of every CTA alike
+    if (csize > 1) cluster_wait();
+    if (warp == 0) {
+        float4 v = make_float4(kNegInf, 0.f, 0.f, 0.f);
+        if (lane < kDtWarps) {
+            const float2 q = s_part[lane];
+            v = make_float4(q.x, q.y, 0.f, 0.f);
+        }
+        auto merge = [&](float4& w) {
+            const float m = warp_reduce(w.x, [](float a, float b) { return fmaxf(a, b); });
+            w.y = warp_reduce(w.y * dt_to_ref(w.x, m), [](float a, float b) { return a + b; });
+            w.x = m;
+        };
+        merge(v);
+        v.z = (s_bad ? 1.f : 0.f) + (failed ? 2.f : 0.f);
+        bool gone = false;
+        float flags = v.z;
+        if (csize > 1) {
+            if (lane < csize)
+                st_async_v4(map_rank(&s_recv[rank], static_cast<uint32_t>(lane)), v, map_rank(&s_peer, static_cast<uint32_t>(lane)));
+            if (lane == 0) mbar_arrive_expect_tx(&s_peer, static_cast<uint32_t>(csize) * 16u);
+            gone = !__all_sync(0xffffffffu, mbar_wait_cluster_bounded(&s_peer, 0, kDtPeerWaitNs));
+            v = make_float4(kNegInf, 0.f, 0.f, 0.f);
+            if (lane < csize && !gone) v = s_recv[lane];
+            flags = warp_reduce(v.z, [](float a, float b) { return fmaxf(a, b); });
+            merge(v);
+        }
+        DtSums r;
+        r.M = v.x;
+        r.S = v.y;
+        const bool others = r.M != kNegInf;
+        // exponents against M: the largest kept logit's (rounded once, after the difference), and the largest of all
+        const float mz = zmax == kNegInf ? kNegInf : (others ? fmaf(zmax, cl, fmaf(zmax, ch, -r.M)) : 0.f);
+        const float mx = fmaxf(others ? 0.f : kNegInf, mz);
+        r.dz = mz - mx;
+        const float Z = fmaf(r.S, others ? ex2(-mx) : 0.f, Zc * dt_to_ref(mz, mx));
+        r.lgZ = log2f(Z);
+        r.inv_Z = 1.f / Z;
+        r.w = others ? ex2(-mx) * r.inv_Z : 0.f;
+        r.qr = r.S * r.w;
+        r.lqr = others ? (log2f(r.S) - mx) - r.lgZ : kNegInf;
+        r.lpr = kKind == OSD_CE ? kNegInf : (tr - mt) - log2f(L);
+        r.pr = kKind == OSD_CE ? 0.f : ex2(tr - mt) / L;
+        r.coef = others ? r.w - (r.pr > 0.f ? r.pr / r.S : 0.f) : 0.f;
+        r.bad = gone || flags >= 2.f ? 2 : (flags > 0.f ? 1 : 0);
+        if (lane == 0) sm = r;
+    }
+    __syncthreads();
+    const DtSums r = sm;
+    const bool dead_row = r.bad || empty;
+    if (r.bad == 2) {  // a copy or a peer's sum did not arrive in time
+        if (tid == 0) {
+            if (rank == 0) p.loss[row] = __int_as_float(0x7fc00000);
+            if (p.status) atomicExch(p.status, static_cast<int32_t>(OSD_ERR_TIMEOUT));
+        }
+        return;
+    }
+    // ---- the classes, by every CTA alike
     const float lgL = log2f(L), inv_L = 1.f / L;
-    // ---- the draft: the sum of the others against their largest, m
-    auto kept = [&](int j) { return (s_bits[j >> 5] >> (j & 31)) & 1u; };
-    float m = kNegInf;
-    for (int j = tid; j < V; j += kDtThreads)
-        if (!kept(j)) m = fmaxf(m, E::load(x + j));
-    m = block_reduce<kDtThreads>(m, most, s_red);
-    const bool others = m != kNegInf;
-    float zmax = kNegInf;
-    for (int i = tid; i < K; i += kDtThreads)
-        if (s_id[i] >= 0) zmax = fmaxf(zmax, s_z[i]);
-    zmax = block_reduce<kDtThreads>(zmax, most, s_red);
-    if (!others) m = zmax;
-    float S = 0.f;
-    if (others)
-        for (int j = tid; j < V; j += kDtThreads)
-            if (!kept(j)) S += ex2((E::load(x + j) - m) * c);
-    S = block_reduce<kDtThreads>(S, add, s_red);
-    const float mx = fmaxf(others ? 0.f : kNegInf, mul_c(zmax - m, ch, cl));
-    float Z = 0.f;
-    for (int i = tid; i < K; i += kDtThreads)
-        if (s_id[i] >= 0) Z += ex2(mul_c(s_z[i] - m, ch, cl) - mx);
-    Z = block_reduce<kDtThreads>(Z, add, s_red) + S * ex2(-mx);
-    const float lgZ = log2f(Z), inv_Z = 1.f / Z;
-    // ---- the classes
-    const float lqr = others ? (log2f(S) - mx) - lgZ : kNegInf, qr = S * ex2(-mx) * inv_Z;
-    const float lpr = kKind == OSD_CE ? kNegInf : (tr - mt) - lgL, pr = kKind == OSD_CE ? 0.f : ex2(tr - mt) * inv_L;
     auto target = [&](int i, float& pc, float& lp) {
         if constexpr (kKind == OSD_CE) {
             pc = s_id[i] == best.i ? 1.f : 0.f;
             lp = pc > 0.f ? 0.f : kNegInf;
         } else {
-            const float t = t_of(i);
-            pc = ex2(t) * inv_L;
-            lp = t - lgL;
+            pc = ex2(s_t[i]) * inv_L;
+            lp = s_t[i] - lgL;
         }
     };
     auto draft = [&](int i, float& qc, float& lq) {
-        const float e = mul_c(s_z[i] - m, ch, cl) - mx;
-        qc = ex2(e) * inv_Z;
-        lq = e - lgZ;
+        const float e = s_e[i] == kNegInf ? kNegInf : s_e[i] + r.dz;
+        qc = ex2(e) * r.inv_Z;
+        lq = e - r.lgZ;
     };
-    float3 s = tid == 0 ? class_terms<kKind>(pr, lpr, qr, lqr, p.beta) : make_float3(0.f, 0.f, 0.f);
-    for (int i = tid; i < K; i += kDtThreads) {
+    float3 s = tid == 0 ? class_terms<kKind>(r.pr, r.lpr, r.qr, r.lqr, p.beta) : make_float3(0.f, 0.f, 0.f);
+    for (int i = tid; i < K; i += kT) {
         if (s_id[i] < 0) continue;
         float pc, lp, qc, lq;
         target(i, pc, lp);
@@ -198,48 +371,89 @@ __global__ void __launch_bounds__(kDtThreads) distill_topk_kernel(DtParams p) {
         const float3 t = class_terms<kKind>(pc, lp, qc, lq, p.beta);
         s = make_float3(s.x + t.x, s.y + t.y, s.z + t.z);
     }
-    s = block_reduce<kDtThreads>(s, [](float3 a, float3 b) { return make_float3(a.x + b.x, a.y + b.y, a.z + b.z); }, s_red3);
+    s = warp_reduce(s, [](float3 a, float3 b) { return make_float3(a.x + b.x, a.y + b.y, a.z + b.z); });
+    if (lane == 0) s_terms[warp] = s;
+    __syncthreads();
+    s = s_terms[0];
+#pragma unroll
+    for (int w = 1; w < kDtWarps; ++w) s = make_float3(s.x + s_terms[w].x, s.y + s_terms[w].y, s.z + s_terms[w].z);
     const float loss = class_loss<kKind>(s, p.beta);
-    if (tid == 0) p.loss[row] = loss;
-    const bool dead = kKind == OSD_RKL && !(loss < __int_as_float(0x7f800000));  // +inf: no gradient
-    // ---- the gradient: others first, then the kept entries over them
+    if (rank == 0 && tid == 0) {
+        p.loss[row] = r.bad ? __int_as_float(0x7fc00000) : (empty ? 0.f : loss);
+        if (r.bad && p.status) atomicExch(p.status, static_cast<int32_t>(OSD_ERR_INVALID_ARG));
+    }
+    // ---- the gradient: the others first, then the kept entries over them
+    const bool dead = dead_row || (kKind == OSD_RKL && !(loss < __int_as_float(0x7f800000)));  // +inf: no gradient
     float coef = 0.f;
-    if (others && !dead) {
-        const float w = ex2(-mx) * inv_Z;
-        if constexpr (kKind == OSD_FKL || kKind == OSD_CE) coef = w - pr / S;  // q_j - p_R q_j / q_R
-        else coef = w * class_factor<kKind>(pr, lpr, qr, lqr, s, loss, p.beta);
+    if (!dead && r.M != kNegInf) {
+        if constexpr (kKind == OSD_FKL || kKind == OSD_CE) coef = r.coef;
+        else coef = r.w * class_factor<kKind>(r.pr, r.lpr, r.qr, r.lqr, s, loss, p.beta);
         coef *= p.inv_tau;
     }
-    for (int j = tid; j < V; j += kDtThreads)
-        if (!kept(j)) out[j] = others ? coef * ex2((E::load(x + j) - m) * c) : 0.f;
-    for (int i = tid; i < K; i += kDtThreads) {
-        if (s_id[i] < 0) continue;
+    const float M = r.M == kNegInf ? 0.f : r.M;
+    auto entry = [&](int at) {  // one staged entry
+        const int j = p0 + at - ph;
+        if (j >= 0 && j < V) out[j] = coef * ex2(fmaf(E::lds(staged + at), c, -M));
+    };
+    // 16-byte stores where the gradient's row has the chunks' phase
+    if ((((reinterpret_cast<uintptr_t>(out) >> 2) - static_cast<unsigned>(ph)) & 3u) == 0) {
+        float* o = out + p0 - ph;
+#pragma unroll 2
+        for (int v = c0 + tid; v < c1; v += kT) {
+            float y[kW];
+            E::unpack(lds_v4(staged + v * kW), y);
+#pragma unroll
+            for (int e = 0; e < kW; e += 4) {
+                float2 a = fma2(make_float2(y[e], y[e + 1]), f2(c), f2(-M)), b = fma2(make_float2(y[e + 2], y[e + 3]), f2(c), f2(-M));
+                a = mul2(make_float2(ex2(a.x), ex2(a.y)), f2(coef));
+                b = mul2(make_float2(ex2(b.x), ex2(b.y)), f2(coef));
+                stg_v4(o + v * kW + e, a.x, a.y, b.x, b.y);
+            }
+        }
+        if (tid < kW) {
+            if (c0 == 1 && n > 0) entry(tid);
+            if (c1 < n && c1 >= c0) entry((n - 1) * kW + tid);
+        }
+    } else {
+        for (int i = tid; i < n * kW; i += kT) entry(i);
+    }
+    __syncthreads();
+    for (int i = tid; i < K; i += kT) {
+        const int id = s_id[i], at = id + ph - p0;
+        if (id < 0 || at < 0 || at >= p1 - p0) continue;
         float pc, lp, qc, lq, g = 0.f;
         target(i, pc, lp);
         draft(i, qc, lq);
-        if constexpr (kKind == OSD_FKL || kKind == OSD_CE) g = qc - pc;
-        else if (qc > 0.f && !dead) g = qc * class_factor<kKind>(pc, lp, qc, lq, s, loss, p.beta);
-        out[s_id[i]] = g * p.inv_tau;
+        if (!dead) {
+            if constexpr (kKind == OSD_FKL || kKind == OSD_CE) g = qc - pc;
+            else if (qc > 0.f) g = qc * class_factor<kKind>(pc, lp, qc, lq, s, loss, p.beta);
+        }
+        out[id] = g * p.inv_tau;
     }
 }
 
 template <typename In>
-static cudaError_t launch_distill_topk(osd_loss kind, const DtParams& dp, unsigned rows, cudaStream_t s) {
-    const size_t smem = size_t((dp.V + 31) / 32) * 4;
-    const dim3 grid(rows), block(kDtThreads);
-    auto go = [&](auto* kernel) -> cudaError_t {
-        if (smem > 24 * 1024) {
-            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDtMaxV / 8);
-            if (e != cudaSuccess) return e;
-        }
-        return launch_ex(true, kernel, grid, block, smem, s, 1, dp);
+static osd_status launch_distill_topk(osd_loss kind, DtParams dp, long long rows, cudaStream_t s) {
+    constexpr size_t es = sizeof(In);
+    const int positions = dp.V + Elem<In>::kVec - 1;  // a row starts up to kVec - 1 positions into the grid
+    int c = static_cast<int>((size_t(positions) * es + DT_SPAN - 1) / DT_SPAN);
+    c = std::max(1, std::min(c, kDtMaxCluster));
+    dp.span = ((positions + c - 1) / c + 63) / 64 * 64;
+    dp.csize = (positions + dp.span - 1) / dp.span;
+    if (rows * dp.csize > INT_MAX) return OSD_ERR_UNSUPPORTED;
+    const size_t smem = size_t(dp.span) * es + size_t(dp.K) * 12 + size_t((dp.span + 31) / 32) * 4;
+    auto go = [&](auto kind_tag) -> osd_status {
+        constexpr int kKind = decltype(kind_tag)::value;
+        if (ctas_per_sm<distill_topk_kernel<In, kKind>, kDtThreads>(smem) < 1) return OSD_ERR_CUDA;  // (opts in for the size)
+        return from_cuda(launch_ex(true, distill_topk_kernel<In, kKind>, dim3(static_cast<unsigned>(rows * dp.csize)),
+                                   dim3(kDtThreads), smem, s, dp.csize, dp));
     };
     switch (kind) {
-        case OSD_FKL: return go(distill_topk_kernel<In, OSD_FKL>);
-        case OSD_RKL: return go(distill_topk_kernel<In, OSD_RKL>);
-        case OSD_JSD: return go(distill_topk_kernel<In, OSD_JSD>);
-        case OSD_TVD: return go(distill_topk_kernel<In, OSD_TVD>);
-        default: return go(distill_topk_kernel<In, OSD_CE>);
+        case OSD_FKL: return go(std::integral_constant<int, OSD_FKL>());
+        case OSD_RKL: return go(std::integral_constant<int, OSD_RKL>());
+        case OSD_JSD: return go(std::integral_constant<int, OSD_JSD>());
+        case OSD_TVD: return go(std::integral_constant<int, OSD_TVD>());
+        default: return go(std::integral_constant<int, OSD_CE>());
     }
 }
 
@@ -276,6 +490,5 @@ extern "C" osd_status osd_distill_topk(const void* draft_logits, osd_dtype dtype
     dp.c = static_cast<float>(1.4426950408889634074 / static_cast<double>(temperature));
     dp.inv_tau = static_cast<float>(1.0 / static_cast<double>(temperature));
     dp.loss = loss; dp.dlogits = dlogits; dp.status = status;
-    return from_cuda(dtype == OSD_BF16 ? launch_distill_topk<__nv_bfloat16>(kind, dp, static_cast<unsigned>(rows), s)
-                                       : launch_distill_topk<float>(kind, dp, static_cast<unsigned>(rows), s));
+    return dtype == OSD_BF16 ? launch_distill_topk<__nv_bfloat16>(kind, dp, rows, s) : launch_distill_topk<float>(kind, dp, rows, s);
 }
