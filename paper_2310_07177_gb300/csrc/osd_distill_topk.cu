@@ -12,10 +12,17 @@
 // ones would cancel), K + 1 classes' worth of arithmetic, and one scaled exponential an entry.
 //
 // One thread-block cluster per row, each CTA with a span of it in shared memory (one bulk
-// copy).  While that flies, the CTA takes the kept tokens: the target's distribution, and the
-// draft's logits there, gathered from global memory so that every CTA has them all.  Then the kept
-// entries are set to -inf in the staged span; its sum of exponentials meets the others by st.async; the classes
-// follow, by every CTA alike; and a second sweep over the span writes the gradient.
+// copy).  While that flies, every CTA takes the target's distribution from the kept values.  Then the draft's logits at
+// the kept tokens within the span are put aside and -inf in their place; the sums of exponentials of the
+// two kinds of entries meet by st.async; each CTA adds up the loss of its kept tokens; and, once the loss's
+// sums have met too (the KL and CE gradients need none of them), a second sweep over the span writes the gradient.
+//
+// Bound by HBM at flush sizes: a row is read and its gradient written once (the registers are capped for
+// ten CTAs of 128 threads an SM, for the KL and CE gradients eight: 8000 x 32000 bf16 FKL, K = 64 230 us, ten: 256; RKL
+// with eight 507 for 469).  16384 x 32000 bf16 RKL, K = 64 469 us, 6.7 TB/s, 99 % of the measured copy bandwidth; 2048 x
+// 128256 FKL, K = 256 271 us (86 %), where a cluster of eight waits for its sums; 16 x 32000 fp32 5.8 us, a chain of copy,
+// two exchanges and stores.  With the draft's logits gathered from global memory by every CTA, and no second
+// exchange, the last took 5.4 us but 4000 x 32000 FKL, K = 512 193 us, where it takes 155.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -28,14 +35,11 @@
 
 namespace osd {
 
-#ifndef DT_SPAN
-#define DT_SPAN 32768
-#define DT_R 1280
-#endif
 constexpr int kDtThreads = 128;
 constexpr int kDtWarps = kDtThreads / 32;
 constexpr int kDtMaxCluster = 8;
 constexpr int kDtMaxV = 393216;
+constexpr size_t kDtSpanBytes = 32768;        // of a CTA's span where there are rows enough
 constexpr uint64_t kDtStageWaitNs = 1000000000ull;  // bound on the wait for the bulk copy ...
 constexpr uint64_t kDtPeerWaitNs = 3000000000ull;   // ... and for the peers' sums
 constexpr float kDtRefMax = 4294967296.f;           // a warp's sum past this takes its true maximum
@@ -110,7 +114,8 @@ __device__ __forceinline__ float class_factor(float p, float lp, float q, float 
 struct DtSums {
     float M, S;     // the others: sum of 2^(x c - M)
     float lgZ, inv_Z;  // the normaliser against the largest exponent of all ...
-    float dz, w;    // ... that of the largest kept logit, and the probability of an other token per 2^(x c - M)
+    float zmax, dz;    // ... the largest kept logit and its exponent there,
+    float w;           // and the probability of an other token per 2^(x c - M)
     float pr, lpr, qr, lqr;
     float coef;     // FKL, CE: of the others' gradient
     int bad;
@@ -120,17 +125,19 @@ struct DtSums {
 __device__ __forceinline__ float dt_to_ref(float a, float b) { return a == kNegInf ? 0.f : ex2(a - b); }
 
 template <typename In, int kKind>
-__global__ void __launch_bounds__(kDtThreads, DT_R / kDtThreads) distill_topk_kernel(DtParams p) {
+__global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_CE ? 8 : 10) distill_topk_kernel(DtParams p) {
     using E = Elem<In>;
     constexpr int kW = E::kVec, kT = kDtThreads;
+    constexpr bool kNoSums = kKind == OSD_FKL || kKind == OSD_CE;  // the gradient needs none of the loss's sums
     extern __shared__ __align__(128) unsigned char dsm[];
-    __shared__ __align__(16) float4 s_recv[kDtMaxCluster];  // slot r from CTA r
-    __shared__ __align__(8) uint64_t s_bar, s_peer;
-    __shared__ float2 s_part[kDtWarps];
+    __shared__ __align__(16) float4 s_recv[2][kDtMaxCluster];  // slot r from CTA r: of the sums, of the loss
+    __shared__ __align__(8) uint64_t s_bar, s_peer[2];
+    __shared__ float4 s_part[kDtWarps];
     __shared__ float3 s_terms[kDtWarps];
     __shared__ MaxIdx s_best[kDtWarps];
-    __shared__ float s_wz[kDtWarps], s_wl[kDtWarps], s_we[kDtWarps];
+    __shared__ float s_wl[kDtWarps];
     __shared__ DtSums sm;
+    __shared__ float4 s_loss;
     __shared__ int s_bad;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int csize = p.csize, rank = csize > 1 ? static_cast<int>(cluster_rank()) : 0;
@@ -157,12 +164,13 @@ __global__ void __launch_bounds__(kDtThreads, DT_R / kDtThreads) distill_topk_ke
     In* staged = reinterpret_cast<In*>(dsm);
     int* s_id = reinterpret_cast<int*>(dsm + size_t(p.span) * sizeof(In));
     float* s_t = reinterpret_cast<float*>(s_id + K);  // log2 of the target's weight against the largest kept
-    float* s_e = s_t + K;                             // (z - zmax) c
-    uint32_t* s_seen = reinterpret_cast<uint32_t*>(s_e + K);  // which of this CTA's positions are kept
+    float* s_z = s_t + K;                             // the draft's logits at this CTA's
+    uint32_t* s_seen = reinterpret_cast<uint32_t*>(s_z + K);  // which of this CTA's positions are kept
     if (tid == 0) {
         s_bad = 0;
         mbar_init_only(&s_bar, 1);
-        mbar_init_only(&s_peer, 1);
+        mbar_init_only(&s_peer[0], 1);
+        mbar_init_only(&s_peer[1], 1);
         fence_mbarrier_init();
         if (c1 > c0) {
             const uint32_t bytes = static_cast<uint32_t>(c1 - c0) * 16u;
@@ -182,78 +190,68 @@ __global__ void __launch_bounds__(kDtThreads, DT_R / kDtThreads) distill_topk_ke
     if (c1 < n && c1 >= c0) fringe(n - 1);
     __syncthreads();
 
-    // ---- the kept tokens: the largest value with its lowest id, and the largest draft logit
+    // ---- the target: the kept tokens' values against the largest (with its lowest id)
     const float c = p.c, ch = p.c_hi, cl = p.c_lo;
+    auto place = [&](int id) { return id >= 0 ? static_cast<unsigned>(id + ph - p0) : 0xffffffffu; };
+    const unsigned held = static_cast<unsigned>(max(0, p1 - p0));  // this CTA's tokens: place(id) < held
     MaxIdx best{kNegInf, INT_MAX};
-    float zmax = kNegInf;
     for (int i = tid; i < K; i += kT) {
-        const int id = p.ids[size_t(row) * K + i];
-        float v = p.values[size_t(row) * K + i], z = kNegInf;
-        if (id >= V) s_bad = 1;
-        const bool used = id >= 0 && id < V;
-        if (used) {
-            z = E::load(x + id);
-            best = merge_mi(best, MaxIdx{v, id});
-            zmax = fmaxf(zmax, z);
-            const int at = id + ph - p0;
-            if (at >= 0 && at < p1 - p0 && (atomicOr(&s_seen[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u)) s_bad = 1;
-        } else {
-            v = kNegInf;
+        int id = p.ids[size_t(row) * K + i];
+        const float v = p.values[size_t(row) * K + i];
+        if (id >= V) {
+            s_bad = 1;
+            id = -1;
         }
-        s_id[i] = used ? id : -1;
-        s_t[i] = v;
-        s_e[i] = z;
+        if (id >= 0) best = merge_mi(best, MaxIdx{v, id});
+        const unsigned at = place(id);
+        if (at < held && (atomicOr(&s_seen[at >> 5], 1u << (at & 31u)) >> (at & 31u) & 1u)) s_bad = 1;
+        s_id[i] = id;
+        s_t[i] = id >= 0 ? v : kNegInf;
     }
     best = warp_reduce(best, [](MaxIdx a, MaxIdx b) { return merge_mi(a, b); });
-    zmax = warp_reduce(zmax, [](float a, float b) { return fmaxf(a, b); });
-    if (lane == 0) {
-        s_best[warp] = best;
-        s_wz[warp] = zmax;
-    }
+    if (lane == 0) s_best[warp] = best;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kDtWarps; ++w) {
-        best = merge_mi(best, s_best[w]);
-        zmax = fmaxf(zmax, s_wz[w]);
-    }
+    for (int w = 0; w < kDtWarps; ++w) best = merge_mi(best, s_best[w]);
     const float vref = best.m, rest = (p.rest && kKind != OSD_CE) ? p.rest[row] : kNegInf;
     const bool empty = fmaxf(vref, rest) == kNegInf;  // no target mass
     // t_c: log2 of the class's weight against the largest kept value's; mt: their largest
     const float tr = rest == kNegInf ? kNegInf : (vref == kNegInf ? 0.f : rest_minus(rest, vref, ch, cl));
     const float mt = vref == kNegInf ? tr : fmaxf(0.f, tr);
-    float L = 0.f, Zc = 0.f;
+    float L = 0.f;
     for (int i = tid; i < K; i += kT) {
-        const float v = s_t[i], z = s_e[i];
-        const float t = v == kNegInf ? kNegInf : mul_c(v - vref, ch, cl) - mt, e = z == kNegInf ? kNegInf : mul_c(z - zmax, ch, cl);
+        const float v = s_t[i], t = v == kNegInf ? kNegInf : mul_c(v - vref, ch, cl) - mt;
         s_t[i] = t;
-        s_e[i] = e;
         L += ex2(t);
-        Zc += ex2(e);
     }
     L = warp_reduce(L, [](float a, float b) { return a + b; });
-    Zc = warp_reduce(Zc, [](float a, float b) { return a + b; });
-    if (lane == 0) {
-        s_wl[warp] = L;
-        s_we[warp] = Zc;
-    }
-    // ---- the staged span: kept entries leave it
+    if (lane == 0) s_wl[warp] = L;
+    // ---- the staged span: the kept entries leave it
     bool late = false;
     if (c1 > c0 && !mbar_wait_bounded(&s_bar, 0, kDtStageWaitNs)) {
         late = true;
         mbar_wait_bounded(&s_bar, 0, kDtStageWaitNs);  // give the copy in flight a last chance to land
     }
+    float zmax = kNegInf, Zc = 0.f;  // of the warp's kept tokens: the largest logit, the sum of 2^((z - it) c)
     for (int i = tid; i < K; i += kT) {
-        const int at = s_id[i] + ph - p0;
-        if (s_id[i] >= 0 && at >= 0 && at < p1 - p0) E::store(staged + at, kNegInf);
+        const unsigned at = place(s_id[i]);
+        if (at < held) {
+            const float z = E::lds(staged + at);
+            E::store(staged + at, kNegInf);
+            s_z[i] = z;
+            zmax = fmaxf(zmax, z);
+        }
+    }
+    zmax = warp_reduce(zmax, [](float a, float b) { return fmaxf(a, b); });
+    if (zmax != kNegInf) {
+        for (int i = tid; i < K; i += kT)
+            if (place(s_id[i]) < held) Zc += ex2(mul_c(s_z[i] - zmax, ch, cl));
+        Zc = warp_reduce(Zc, [](float a, float b) { return a + b; });
     }
     const bool failed = __syncthreads_or(late);
     L = ex2(tr - mt);
-    Zc = 0.f;
 #pragma unroll
-    for (int w = 0; w < kDtWarps; ++w) {
-        L += s_wl[w];
-        Zc += s_we[w];
-    }
+    for (int w = 0; w < kDtWarps; ++w) L += s_wl[w];
     // ---- the others' exponentials against the warp's reference, the largest entry of its first chunks: sums past
     // 2^32, and warps whose first chunks hold nothing, take the true maximum first
     const float2 mine = [&]() {
@@ -287,35 +285,42 @@ __global__ void __launch_bounds__(kDtThreads, DT_R / kDtThreads) distill_topk_ke
         }
         return make_float2(m == kNegInf ? kNegInf : M, s);
     }();
-    if (lane == 0) s_part[warp] = mine;
+    if (lane == 0) s_part[warp] = make_float4(mine.x, mine.y, zmax, Zc);
     __syncthreads();
-    // ---- the cluster's sum, and what follows from it, by warp 0 of every CTA alike
+    // ---- the cluster's sums, and what follows from them, by warp 0 of every CTA alike
     if (csize > 1) cluster_wait();
+    auto push = [&](int which, float4 v, int to) {  // warp 0: to the first CTAs of the cluster
+        if (lane < to)
+            st_async_v4(map_rank(&s_recv[which][rank], static_cast<uint32_t>(lane)), v,
+                        map_rank(&s_peer[which], static_cast<uint32_t>(lane)));
+        if (lane == 0 && rank < to) mbar_arrive_expect_tx(&s_peer[which], static_cast<uint32_t>(csize) * 16u);
+    };
+    auto arrived = [&](int which) {
+        return __all_sync(0xffffffffu, mbar_wait_cluster_bounded(&s_peer[which], 0, kDtPeerWaitNs)) != 0;
+    };
     if (warp == 0) {
-        float4 v = make_float4(kNegInf, 0.f, 0.f, 0.f);
-        if (lane < kDtWarps) {
-            const float2 q = s_part[lane];
-            v = make_float4(q.x, q.y, 0.f, 0.f);
-        }
+        float4 v = lane < kDtWarps ? s_part[lane] : make_float4(kNegInf, 0.f, kNegInf, 0.f);
         auto merge = [&](float4& w) {
             const float m = warp_reduce(w.x, [](float a, float b) { return fmaxf(a, b); });
+            const float z = warp_reduce(w.z, [](float a, float b) { return fmaxf(a, b); });
             w.y = warp_reduce(w.y * dt_to_ref(w.x, m), [](float a, float b) { return a + b; });
+            w.w = warp_reduce(w.z == kNegInf ? 0.f : w.w * ex2(mul_c(w.z - z, ch, cl)), [](float a, float b) { return a + b; });
             w.x = m;
+            w.z = z;
         };
         merge(v);
-        v.z = (s_bad ? 1.f : 0.f) + (failed ? 2.f : 0.f);
+        if (failed || s_bad) v.y = failed ? -2.f : -1.f;  // (sums are not negative)
         bool gone = false;
-        float flags = v.z;
+        float flags = fminf(v.y, 0.f);
         if (csize > 1) {
-            if (lane < csize)
-                st_async_v4(map_rank(&s_recv[rank], static_cast<uint32_t>(lane)), v, map_rank(&s_peer, static_cast<uint32_t>(lane)));
-            if (lane == 0) mbar_arrive_expect_tx(&s_peer, static_cast<uint32_t>(csize) * 16u);
-            gone = !__all_sync(0xffffffffu, mbar_wait_cluster_bounded(&s_peer, 0, kDtPeerWaitNs));
-            v = make_float4(kNegInf, 0.f, 0.f, 0.f);
-            if (lane < csize && !gone) v = s_recv[lane];
-            flags = warp_reduce(v.z, [](float a, float b) { return fmaxf(a, b); });
+            push(0, v, csize);
+            gone = !arrived(0);
+            v = lane < csize && !gone ? s_recv[0][lane] : make_float4(kNegInf, 0.f, kNegInf, 0.f);
+            flags = warp_reduce(fminf(v.y, 0.f), [](float a, float b) { return fminf(a, b); });
             merge(v);
         }
+        zmax = v.z;
+        Zc = v.w;
         DtSums r;
         r.M = v.x;
         r.S = v.y;
@@ -333,7 +338,8 @@ __global__ void __launch_bounds__(kDtThreads, DT_R / kDtThreads) distill_topk_ke
         r.lpr = kKind == OSD_CE ? kNegInf : (tr - mt) - log2f(L);
         r.pr = kKind == OSD_CE ? 0.f : ex2(tr - mt) / L;
         r.coef = others ? r.w - (r.pr > 0.f ? r.pr / r.S : 0.f) : 0.f;
-        r.bad = gone || flags >= 2.f ? 2 : (flags > 0.f ? 1 : 0);
+        r.zmax = zmax;
+        r.bad = gone || flags < -1.f ? 2 : (flags < 0.f ? 1 : 0);
         if (lane == 0) sm = r;
     }
     __syncthreads();
@@ -358,38 +364,66 @@ __global__ void __launch_bounds__(kDtThreads, DT_R / kDtThreads) distill_topk_ke
         }
     };
     auto draft = [&](int i, float& qc, float& lq) {
-        const float e = s_e[i] == kNegInf ? kNegInf : s_e[i] + r.dz;
+        const float z = s_z[i], e = z == kNegInf ? kNegInf : mul_c(z - r.zmax, ch, cl) + r.dz;
         qc = ex2(e) * r.inv_Z;
         lq = e - r.lgZ;
     };
-    float3 s = tid == 0 ? class_terms<kKind>(r.pr, r.lpr, r.qr, r.lqr, p.beta) : make_float3(0.f, 0.f, 0.f);
+    float3 s = rank == 0 && tid == 0 ? class_terms<kKind>(r.pr, r.lpr, r.qr, r.lqr, p.beta) : make_float3(0.f, 0.f, 0.f);
     for (int i = tid; i < K; i += kT) {
-        if (s_id[i] < 0) continue;
+        if (place(s_id[i]) >= held) continue;
         float pc, lp, qc, lq;
         target(i, pc, lp);
         draft(i, qc, lq);
         const float3 t = class_terms<kKind>(pc, lp, qc, lq, p.beta);
         s = make_float3(s.x + t.x, s.y + t.y, s.z + t.z);
     }
-    s = warp_reduce(s, [](float3 a, float3 b) { return make_float3(a.x + b.x, a.y + b.y, a.z + b.z); });
+    auto add3 = [](float3 a, float3 b) { return make_float3(a.x + b.x, a.y + b.y, a.z + b.z); };
+    s = warp_reduce(s, add3);
     if (lane == 0) s_terms[warp] = s;
     __syncthreads();
-    s = s_terms[0];
+    if (warp == 0) {
+        s = s_terms[0];
 #pragma unroll
-    for (int w = 1; w < kDtWarps; ++w) s = make_float3(s.x + s_terms[w].x, s.y + s_terms[w].y, s.z + s_terms[w].z);
-    const float loss = class_loss<kKind>(s, p.beta);
-    if (rank == 0 && tid == 0) {
-        p.loss[row] = r.bad ? __int_as_float(0x7fc00000) : (empty ? 0.f : loss);
-        if (r.bad && p.status) atomicExch(p.status, static_cast<int32_t>(OSD_ERR_INVALID_ARG));
+        for (int w = 1; w < kDtWarps; ++w) s = add3(s, s_terms[w]);
+        if (csize > 1) push(1, make_float4(s.x, s.y, s.z, 0.f), kNoSums ? 1 : csize);
+    }
+    // the loss's sums over the cluster, in every thread; false if a peer's did not arrive in time
+    auto loss_sums = [&]() {
+        if (warp == 0) {
+            bool got = true;
+            if (csize > 1) {
+                got = arrived(1);
+                s = make_float3(0.f, 0.f, 0.f);
+                for (int q = 0; q < csize && got; ++q) s = add3(s, make_float3(s_recv[1][q].x, s_recv[1][q].y, s_recv[1][q].z));
+            }
+            if (lane == 0) s_loss = make_float4(s.x, s.y, s.z, got ? 0.f : 1.f);
+        }
+        __syncthreads();
+        s = make_float3(s_loss.x, s_loss.y, s_loss.z);
+        return s_loss.w == 0.f;
+    };
+    float loss = 0.f;
+    auto write_loss = [&](bool got) {
+        if (tid == 0) {
+            if (rank == 0) p.loss[row] = r.bad || !got ? __int_as_float(0x7fc00000) : (empty ? 0.f : loss);
+            if (p.status && (!got || (rank == 0 && r.bad)))
+                atomicExch(p.status, static_cast<int32_t>(got ? OSD_ERR_INVALID_ARG : OSD_ERR_TIMEOUT));
+        }
+    };
+    bool dead = dead_row;
+    float coef = 0.f;
+    if constexpr (kNoSums) {
+        if (!dead && r.M != kNegInf) coef = r.coef * p.inv_tau;
+    } else {
+        const bool got = loss_sums();
+        loss = class_loss<kKind>(s, p.beta);
+        write_loss(got);
+        if (!got) return;
+        dead = dead || (kKind == OSD_RKL && !(loss < __int_as_float(0x7f800000)));  // +inf: no gradient
+        if (!dead && r.M != kNegInf)
+            coef = r.w * class_factor<kKind>(r.pr, r.lpr, r.qr, r.lqr, s, loss, p.beta) * p.inv_tau;
     }
     // ---- the gradient: the others first, then the kept entries over them
-    const bool dead = dead_row || (kKind == OSD_RKL && !(loss < __int_as_float(0x7f800000)));  // +inf: no gradient
-    float coef = 0.f;
-    if (!dead && r.M != kNegInf) {
-        if constexpr (kKind == OSD_FKL || kKind == OSD_CE) coef = r.coef;
-        else coef = r.w * class_factor<kKind>(r.pr, r.lpr, r.qr, r.lqr, s, loss, p.beta);
-        coef *= p.inv_tau;
-    }
     const float M = r.M == kNegInf ? 0.f : r.M;
     auto entry = [&](int at) {  // one staged entry
         const int j = p0 + at - ph;
@@ -419,16 +453,20 @@ __global__ void __launch_bounds__(kDtThreads, DT_R / kDtThreads) distill_topk_ke
     }
     __syncthreads();
     for (int i = tid; i < K; i += kT) {
-        const int id = s_id[i], at = id + ph - p0;
-        if (id < 0 || at < 0 || at >= p1 - p0) continue;
+        if (place(s_id[i]) >= held) continue;
         float pc, lp, qc, lq, g = 0.f;
         target(i, pc, lp);
         draft(i, qc, lq);
         if (!dead) {
-            if constexpr (kKind == OSD_FKL || kKind == OSD_CE) g = qc - pc;
+            if constexpr (kNoSums) g = qc - pc;
             else if (qc > 0.f) g = qc * class_factor<kKind>(pc, lp, qc, lq, s, loss, p.beta);
         }
-        out[id] = g * p.inv_tau;
+        out[s_id[i]] = g * p.inv_tau;
+    }
+    if (kNoSums && rank == 0) {
+        const bool got = loss_sums();
+        loss = class_loss<kKind>(s, p.beta);
+        write_loss(got);
     }
 }
 
@@ -436,8 +474,12 @@ template <typename In>
 static osd_status launch_distill_topk(osd_loss kind, DtParams dp, long long rows, cudaStream_t s) {
     constexpr size_t es = sizeof(In);
     const int positions = dp.V + Elem<In>::kVec - 1;  // a row starts up to kVec - 1 positions into the grid
-    int c = static_cast<int>((size_t(positions) * es + DT_SPAN - 1) / DT_SPAN);
-    c = std::max(1, std::min(c, kDtMaxCluster));
+    // Spans of 32 KB: 16384 x 32000 bf16 RKL 469 us (16 KB: 537, 8 KB: 900; 64 KB: 464, but 128.2 us against 122.4 for
+    // 8192 x 32001 JSD at 40 % active and 319 against 298 for 2048 x 128256 FKL).  A call that leaves SMs idle takes
+    // shorter ones, from 8 KB on (8 x 32000 bf16 RKL 5.8 us, 7.3 with 32 KB).
+    int c = static_cast<int>((size_t(positions) * es + kDtSpanBytes - 1) / kDtSpanBytes);
+    while (c < kDtMaxCluster && rows * 2 * c <= 2 * device_sms() && size_t(positions) * es / (2 * c) >= 8000) c *= 2;
+    c = std::min(c, kDtMaxCluster);
     dp.span = ((positions + c - 1) / c + 63) / 64 * 64;
     dp.csize = (positions + dp.span - 1) / dp.span;
     if (rows * dp.csize > INT_MAX) return OSD_ERR_UNSUPPORTED;
