@@ -4,7 +4,7 @@
 //
 // One thread-block cluster per row, which is read once but for a few groups of entries:
 //
-//   sweep    every thread takes eight groups of 16-byte chunks and keeps each group's
+//   sweep    every thread takes eight or sixteen groups of 16-byte chunks and keeps each group's
 //            maximum and sum of exponentials;
 //   theta    a value that K group maxima reach and few more, from a histogram of them: at
 //            least K entries are theta or larger, and few more where large entries lie
@@ -18,7 +18,11 @@
 // crowded in few groups) go on to the exact K-th largest value, from histograms of all entries,
 // and take the entries equal to it in index order.
 //
-// @@
+// Not bound by one thing: 4096 x 32000 bf16, K = 64 takes 70 us, 3.8 TB/s, with half of the issue slots in use.  A
+// CTA loads for about half of its life (the sweep); theta, the second reading and the ranking are short dependent steps
+// on little data, which ten CTAs an SM overlap.  fp32, twice the bytes an entry, comes nearer to HBM: 4096 x 32001, K = 16
+// 91 us, 5.8 TB/s.  Measured and left out: the row staged in shared memory by a bulk copy (three CTAs an SM: 92 to 102 us),
+// the whole row read twice (95), a prefetch of the row into L2 (74).
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -32,7 +36,6 @@
 namespace osd {
 
 constexpr int kTopMaxCluster = 8;
-constexpr int kTopGroups = 8;        // groups of chunks per thread
 constexpr int kTopBins = 256;        // bins of a histogram over a range of keys
 constexpr int kTopCountMost = 192;   // candidates ranked by counting; more by a histogram of their values
 constexpr int kTopCrowd = 48;        // candidates of one bin that are ranked by comparing; with more all are sorted
@@ -56,7 +59,7 @@ struct TopParams {
     int csize;   // CTAs per row
     int span;    // positions per CTA: whole chunks
     int room;    // candidates a CTA can hold, a power of two
-    int maxima;  // maxima per thread that theta is found from: 1, 2, 4 or 8
+    int maxima;  // maxima per thread that theta is found from, a power of two
 };
 
 // Unsigned keys in the order of the floats; -0 and 0 have the same.
@@ -126,10 +129,10 @@ template <> struct ChunkMax<__nv_bfloat16> {
     __device__ __forceinline__ float top() const { return fmaxf(bf16_lo(m), bf16_hi(m)); }
 };
 
-template <typename In, bool kRest, int kT, bool kFew>
+template <typename In, bool kRest, int kT, int kG, bool kFew>
 __global__ void __launch_bounds__(kT, kFew ? 1 : (kT == 128 ? 1280 : 1024) / kT) topk_kernel(TopParams p) {
     using E = Elem<In>;
-    constexpr int kW = E::kVec, kWarps = kT / 32, kG = kTopGroups;
+    constexpr int kW = E::kVec, kWarps = kT / 32;
     extern __shared__ __align__(128) unsigned char dsm[];
     __shared__ __align__(16) TopSmem<kWarps> sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -158,14 +161,14 @@ __global__ void __launch_bounds__(kT, kFew ? 1 : (kT == 128 ? 1280 : 1024) / kT)
     auto single = [&](int i) { return i < head - first ? first + i : tail + (i - (head - first)); };
     auto load = [&](int v) { return ldg_stream(body + size_t(v) * kW); };
     unsigned long long* cand = reinterpret_cast<unsigned long long*>(dsm);
-    unsigned long long* sorted = cand + p.room;
-    uint32_t* maxima = reinterpret_cast<uint32_t*>(sorted + p.room);
+    unsigned long long* sorted = cand + p.room;  // in place of the lists of chunks
+    uint32_t* chunk_lists = reinterpret_cast<uint32_t*>(sorted);
+    uint32_t* maxima = chunk_lists + 2 * p.room;
     // per warp: its groups, and its chunks, with an entry from theta on
     const int chunk_room = 2 * p.room / kWarps;
-    uint32_t* chunk_lists = maxima + csize * kT * p.maxima;
     uint32_t* chunk_list = chunk_lists + warp * chunk_room;
-    unsigned short* place = reinterpret_cast<unsigned short*>(chunk_lists + 2 * p.room);
-    unsigned char* list = reinterpret_cast<unsigned char*>(place + p.room) + warp * (32 * kG);
+    unsigned short* place = reinterpret_cast<unsigned short*>(maxima + csize * kT * p.maxima);
+    unsigned short* list = place + p.room + warp * (32 * kG);
     if (tid == 0) {
         sh.n = 0;
         sh.left = 0ull;
@@ -195,7 +198,7 @@ __global__ void __launch_bounds__(kT, kFew ? 1 : (kT == 128 ? 1280 : 1024) / kT)
         return d[0].x + d[0].y;
     };
     const int v0 = c0 + tid;
-    constexpr int kHalf = kFew ? kG : kG / 2;  // loads in flight
+    constexpr int kHalf = kFew ? 8 : 4;  // loads in flight
     for (int v = v0; v < c1; v += kG * kT) {
 #pragma unroll
         for (int h = 0; h < kG; h += kHalf) {
@@ -364,7 +367,7 @@ __global__ void __launch_bounds__(kT, kFew ? 1 : (kT == 128 ? 1280 : 1024) / kT)
             const bool is = v0 + i * kT < c1 && (gmax[i].top() >= theta || far || (kRest && !(gsum[i] < 0x1p100f)));
             if (kRest && !is) S = fmaf(gsum[i], scale, S);
             const unsigned m = __ballot_sync(0xffffffffu, is);
-            if (is) list[hits + __popc(m & ((1u << lane) - 1u))] = static_cast<unsigned char>(lane * kG + i);
+            if (is) list[hits + __popc(m & ((1u << lane) - 1u))] = static_cast<unsigned short>(lane * kG + i);
             hits += __popc(m);
         }
         __syncwarp();
@@ -726,7 +729,7 @@ __global__ void __launch_bounds__(kT, kFew ? 1 : (kT == 128 ? 1280 : 1024) / kT)
     }
 }
 
-template <typename In, int kT, bool kFew>
+template <typename In, int kT, int kG, bool kFew>
 static osd_status launch_topk(TopParams tp, long long rows, int c, cudaStream_t s) {
     const int positions = tp.V + Elem<In>::kVec - 1;  // a row starts up to kVec - 1 positions into the grid
     c = std::max(1, std::min(c, kTopMaxCluster));
@@ -735,13 +738,13 @@ static osd_status launch_topk(TopParams tp, long long rows, int c, cudaStream_t 
     tp.room = 256;
     while (tp.room < tp.K + tp.K / 2 + 128) tp.room *= 2;
     tp.maxima = 1;
-    while (tp.maxima < kTopGroups && tp.csize * kT * tp.maxima < 4 * tp.K) tp.maxima *= 2;
-    const size_t smem = size_t(tp.room) * 26 + size_t(tp.csize) * kT * tp.maxima * 4 + size_t(kT) * kTopGroups;
+    while (tp.maxima < kG && tp.csize * kT * tp.maxima < 4 * tp.K) tp.maxima *= 2;
+    const size_t smem = size_t(tp.room) * 18 + size_t(tp.csize) * kT * tp.maxima * 4 + size_t(kT) * kG * 2;
     if (rows * tp.csize > INT_MAX) return OSD_ERR_UNSUPPORTED;
     auto go = [&](auto kernel_tag) -> osd_status {
         constexpr bool kRest = decltype(kernel_tag)::value;
-        if (ctas_per_sm<topk_kernel<In, kRest, kT, kFew>, kT>(smem) < 1) return OSD_ERR_CUDA;  // (opts in for the size)
-        return from_cuda(launch_ex(true, topk_kernel<In, kRest, kT, kFew>, dim3(static_cast<unsigned>(rows * tp.csize)), dim3(kT),
+        if (ctas_per_sm<topk_kernel<In, kRest, kT, kG, kFew>, kT>(smem) < 1) return OSD_ERR_CUDA;  // (opts in for the size)
+        return from_cuda(launch_ex(true, topk_kernel<In, kRest, kT, kG, kFew>, dim3(static_cast<unsigned>(rows * tp.csize)), dim3(kT),
                                    smem, s, tp.csize, tp));
     };
     return tp.rest ? go(std::true_type()) : go(std::false_type());
@@ -750,18 +753,25 @@ static osd_status launch_topk(TopParams tp, long long rows, int c, cudaStream_t 
 template <typename In>
 static osd_status launch_topk_dtype(const TopParams& tp, long long rows, cudaStream_t s) {
     const int chunks = static_cast<int>((tp.V + Elem<In>::kVec - 1) / Elem<In>::kVec);
-    // about 16 to 64 chunks a thread; calls that leave SMs idle take more threads a row, while each has 4
-    // chunks or more, and then more CTAs.  (@@)
+    // About 16 to 64 chunks a thread: 4096 x 4000 bf16, K = 16 17.5 us with 64 threads a row, 28 with 128; 4096 x 32000,
+    // K = 64 70 us with 128 (64: 89, 256: 82); 1024 x 128256, K = 64 68 us with 128 or 256 (64: 114).  More with a large K
+    // (4096 x 32001, K = 256 109 us, 125 with 128), and where a call leaves SMs idle, while each thread has 4 chunks or more: 512
+    // x 32001, K = 16 12.6 us with 256 threads, 15.7 with 128; and then several CTAs a row: 8 x 128256, K = 16 7.8 us with
+    // four of 512 threads, 10.9 with one.
     const long long slots = (long long)device_sms() * 1024;
     int t = chunks <= 1024 ? 64 : (chunks <= 8192 ? 128 : (chunks <= 24576 ? 256 : 512)), c = 1;
-    while (t < 512 && (rows * 2 * t <= slots || t < tp.K) && chunks >= 8 * t) t *= 2;
+    while (t < 512 && ((rows * 2 * t <= slots && chunks >= 8 * t) || (t < tp.K && chunks >= 24 * t))) t *= 2;
     while (c < kTopMaxCluster && rows * 2 * t * c <= slots && chunks > 12 * t * c) c *= 2;
-    if (t == 512 && rows * c <= device_sms() * (tp.mask ? 2 : 1)) return launch_topk<In, 512, true>(tp, rows, c, s);
+    if (t == 512 && rows * c <= device_sms() * (tp.mask ? 2 : 1)) return launch_topk<In, 512, 8, true>(tp, rows, c, s);
+    // sixteen groups a thread halve what is read again, which is much with a large K: 256 x 4 x 128256 fp32, K = 256
+    // 121 us, 128 with eight; but 4096 x 32000 bf16, K = 64 72 us, 70 with eight
+    if (tp.K > 128 && chunks > 8 * t && t >= 256)
+        return t == 256 ? launch_topk<In, 256, 16, false>(tp, rows, c, s) : launch_topk<In, 512, 16, false>(tp, rows, c, s);
     switch (t) {
-        case 64: return launch_topk<In, 64, false>(tp, rows, c, s);
-        case 128: return launch_topk<In, 128, false>(tp, rows, c, s);
-        case 256: return launch_topk<In, 256, false>(tp, rows, c, s);
-        default: return launch_topk<In, 512, false>(tp, rows, c, s);
+        case 64: return launch_topk<In, 64, 8, false>(tp, rows, c, s);
+        case 128: return launch_topk<In, 128, 8, false>(tp, rows, c, s);
+        case 256: return launch_topk<In, 256, 8, false>(tp, rows, c, s);
+        default: return launch_topk<In, 512, 8, false>(tp, rows, c, s);
     }
 }
 
