@@ -54,8 +54,7 @@ struct DtParams {
     int K;
     const uint8_t* mask;
     float beta;
-    float c;           // log2(e) / tau
-    float c_hi, c_lo;  // the same as a pair, for the K + 1 classes
+    float c_hi, c_lo;  // log2(e) / tau as a pair
     float inv_tau;
     float* loss;
     float* dlogits;
@@ -191,7 +190,10 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
     __syncthreads();
 
     // ---- the target: the kept tokens' values against the largest (with its lowest id)
-    const float c = p.c, ch = p.c_hi, cl = p.c_lo;
+    const float ch = p.c_hi, cl = p.c_lo;
+    // x c - M of two entries: one rounding after the cancellation, and one of the rest of c, without which the
+    // others would weigh up to 5e-7 more or less against the kept tokens
+    auto exponents = [ch, cl](float2 x, float M) { return fma2(x, f2(cl), fma2(x, f2(ch), f2(-M))); };
     auto place = [&](int id) { return id >= 0 ? static_cast<unsigned>(id + ph - p0) : 0xffffffffu; };
     const unsigned held = static_cast<unsigned>(max(0, p1 - p0));  // this CTA's tokens: place(id) < held
     MaxIdx best{kNegInf, INT_MAX};
@@ -260,7 +262,7 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
         float M, s;
         for (int pass = 0;; ++pass) {
             m = warp_reduce(m, [](float a, float b) { return fmaxf(a, b); });
-            M = m == kNegInf ? 0.f : __fmul_rn(m, c);
+            M = m == kNegInf ? 0.f : __fmul_rn(m, ch);
             float2 acc = f2(0.f);
 #pragma unroll 2
             for (int v = tid; v < n; v += kT) {
@@ -269,7 +271,7 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
                 float2 d[kW / 2];
 #pragma unroll
                 for (int e = 0; e < kW / 2; ++e) {
-                    const float2 a = fma2(make_float2(y[2 * e], y[2 * e + 1]), f2(c), f2(-M));
+                    const float2 a = exponents(make_float2(y[2 * e], y[2 * e + 1]), M);
                     d[e] = make_float2(ex2(a.x), ex2(a.y));
                 }
 #pragma unroll
@@ -427,7 +429,7 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
     const float M = r.M == kNegInf ? 0.f : r.M;
     auto entry = [&](int at) {  // one staged entry
         const int j = p0 + at - ph;
-        if (j >= 0 && j < V) out[j] = coef * ex2(fmaf(E::lds(staged + at), c, -M));
+        if (j >= 0 && j < V) out[j] = coef * ex2(exponents(f2(E::lds(staged + at)), M).x);
     };
     // 16-byte stores where the gradient's row has the chunks' phase
     if ((((reinterpret_cast<uintptr_t>(out) >> 2) - static_cast<unsigned>(ph)) & 3u) == 0) {
@@ -438,7 +440,7 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
             E::unpack(lds_v4(staged + v * kW), y);
 #pragma unroll
             for (int e = 0; e < kW; e += 4) {
-                float2 a = fma2(make_float2(y[e], y[e + 1]), f2(c), f2(-M)), b = fma2(make_float2(y[e + 2], y[e + 3]), f2(c), f2(-M));
+                float2 a = exponents(make_float2(y[e], y[e + 1]), M), b = exponents(make_float2(y[e + 2], y[e + 3]), M);
                 a = mul2(make_float2(ex2(a.x), ex2(a.y)), f2(coef));
                 b = mul2(make_float2(ex2(b.x), ex2(b.y)), f2(coef));
                 stg_v4(o + v * kW + e, a.x, a.y, b.x, b.y);
@@ -529,7 +531,6 @@ extern "C" osd_status osd_distill_topk(const void* draft_logits, osd_dtype dtype
     dp.draft = draft_logits; dp.P = P; dp.V = V; dp.dsg = d_stride_g; dp.dsp = d_stride_p;
     dp.values = values; dp.ids = ids; dp.rest = rest; dp.K = K; dp.mask = mask; dp.beta = beta;
     split_scale(temperature, &dp.c_hi, &dp.c_lo);
-    dp.c = static_cast<float>(1.4426950408889634074 / static_cast<double>(temperature));
     dp.inv_tau = static_cast<float>(1.0 / static_cast<double>(temperature));
     dp.loss = loss; dp.dlogits = dlogits; dp.status = status;
     return dtype == OSD_BF16 ? launch_distill_topk<__nv_bfloat16>(kind, dp, rows, s) : launch_distill_topk<float>(kind, dp, rows, s);
