@@ -371,58 +371,85 @@ __global__ void __launch_bounds__(kT, kFew ? 1 : (kT == 128 ? 1280 : 1024) / kT)
             hits += __popc(m);
         }
         __syncwarp();
-        // the chunks of these groups, a group a lane: those below theta join the sum, the others a second list
-        // (where a group is one chunk, the list is that of the groups)
-        const bool lone = c1 - c0 <= kG * kT;
-        int chunks = lone ? hits : 0;
-        for (int i0 = 0; i0 < hits && !lone; i0 += 32) {
-            const int at = i0 + lane < hits ? list[i0 + lane] : -1;
-            const int w0 = c0 + warp * 32 + at / kG + (at % kG) * kT;
-            for (int b = c0; b < c1; b += 4 * kG * kT) {
-                uint4 raw[4];
-                bool in[4];
+        // the chunks of these groups, dealt out to the lanes: those below theta join the sum, the others a second
+        // list (where a group is one chunk, the list is that of the groups)
+        const int deep = (c1 - c0 + kG * kT - 1) / (kG * kT);  // chunks of a group at most
+        auto chunk_of = [&](int at, int j) { return c0 + warp * 32 + at / kG + (at % kG + j * kG) * kT; };
+        int chunks = deep == 1 ? hits : 0;
+        if (deep > 1) {
+            const int items = hits * deep;
+            const float inv = 1.f / static_cast<float>(deep);
+            for (int i0 = 0; i0 < items; i0 += 64) {
+                uint4 raw[2];
+                int v[2];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int v = w0 + (b - c0) + u * (kG * kT);
-                    in[u] = at >= 0 && v < c1;
+                for (int u = 0; u < 2; ++u) {
+                    const int i = i0 + u * 32 + lane;
+                    const int h = static_cast<int>((static_cast<float>(i) + 0.5f) * inv);  // i / deep: both are small
                     raw[u] = ninf_raw<In>();
-                    if (in[u]) raw[u] = ldg_nc(body + size_t(v) * kW);
+                    v[u] = i < items ? chunk_of(list[h], i - h * deep) : c1;
+                    if (v[u] < c1) raw[u] = ldg_nc(body + size_t(v[u]) * kW);
                 }
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    if (b + u * (kG * kT) >= c1) break;
-                    const bool is = in[u] && E::max_raw(raw[u]) >= theta;
+                for (int u = 0; u < 2; ++u) {
+                    if (i0 + u * 32 >= items) break;
+                    const bool in = v[u] < c1, is = in && E::max_raw(raw[u]) >= theta;
                     if constexpr (kRest) {
                         const float e = exps(raw[u], Mt);
-                        if (in[u] && !is) S += e;
+                        if (in && !is) S += e;
                     }
                     const unsigned m = __ballot_sync(0xffffffffu, is);
                     if (is) {
                         const int to = chunks + __popc(m & ((1u << lane) - 1u));
-                        if (to < chunk_room) chunk_list[to] = static_cast<uint32_t>(w0 + (b - c0) + u * (kG * kT));
+                        if (to < chunk_room) chunk_list[to] = static_cast<uint32_t>(v[u]);
                     }
                     chunks += __popc(m);
                 }
             }
-        }
-        if (!lone) {
             over = chunks > chunk_room;
             chunks = min(chunks, chunk_room);
         }
         __syncwarp();
-        // and their entries, a chunk a lane, with those outside whole chunks
-        auto entry = [&](float y, int j) {
-            if (y >= theta) append(y, j);
-            else if (kRest) S += ex2(fmaf(y, c, -Mt));
-        };
-        for (int i = lane; i < chunks; i += 32) {
-            const int v = lone ? c0 + warp * 32 + list[i] / kG + (list[i] % kG) * kT : static_cast<int>(chunk_list[i]);
+        // and their entries, a chunk a lane: a place in the candidates for a warp's at a time
+        for (int i0 = 0; i0 < chunks; i0 += 32) {
+            const int i = i0 + lane;
+            const bool in = i < chunks;
+            const int v = !in ? c0 : (deep == 1 ? chunk_of(list[i], 0) : static_cast<int>(chunk_list[i]));
             float y[kW];
-            E::unpack(ldg_nc(body + size_t(v) * kW), y);
+            E::unpack(in ? ldg_nc(body + size_t(v) * kW) : ninf_raw<In>(), y);
+            unsigned mask = 0u;
 #pragma unroll
-            for (int e = 0; e < kW; ++e) entry(y[e], v * kW + e - ph);
+            for (int e = 0; e < kW; ++e) {
+                const bool is = in && y[e] >= theta;
+                mask |= is ? 1u << e : 0u;
+                if constexpr (kRest) {
+                    const float q = ex2(fmaf(y[e], c, -Mt));
+                    if (in && !is) S += q;
+                }
+            }
+            int at = __popc(mask);
+            const int mine = at;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int z = __shfl_up_sync(0xffffffffu, at, o);
+                if (lane >= o) at += z;
+            }
+            int from = 0;
+            if (lane == 31) from = atomicAdd(&sh.n, at);
+            at += __shfl_sync(0xffffffffu, from, 31) - mine;
+#pragma unroll
+            for (int e = 0; e < kW; ++e) {
+                if (mask >> e & 1u) {
+                    if (at < p.room) cand[at] = cand_of(y[e], v * kW + e - ph);
+                    ++at;
+                }
+            }
         }
-        if (tid < singles) entry(E::load(x + single(tid)), single(tid));
+        if (tid < singles) {  // the entries outside whole chunks
+            const float y = E::load(x + single(tid));
+            if (y >= theta) append(y, single(tid));
+            else if (kRest) S += ex2(fmaf(y, c, -Mt));
+        }
     }
     if (over && lane == 0) atomicAdd(&sh.n, 1 << 24);  // (above any room)
     if constexpr (kRest) {
@@ -759,7 +786,7 @@ static osd_status launch_topk_dtype(const TopParams& tp, long long rows, cudaStr
     // x 32001, K = 16 12.6 us with 256 threads, 15.7 with 128; and then several CTAs a row: 8 x 128256, K = 16 7.8 us with
     // four of 512 threads, 10.9 with one.
     const long long slots = (long long)device_sms() * 1024;
-    int t = chunks <= 1024 ? 64 : (chunks <= 8192 ? 128 : (chunks <= 24576 ? 256 : 512)), c = 1;
+    int t = chunks <= 2048 ? 64 : (chunks <= 8192 ? 128 : (chunks <= 24576 ? 256 : 512)), c = 1;
     while (t < 512 && ((rows * 2 * t <= slots && chunks >= 8 * t) || (t < tp.K && chunks >= 24 * t))) t *= 2;
     while (c < kTopMaxCluster && rows * 2 * t * c <= slots && chunks > 12 * t * c) c *= 2;
     if (t == 512 && rows * c <= device_sms() * (tp.mask ? 2 : 1)) return launch_topk<In, 512, 8, true>(tp, rows, c, s);
