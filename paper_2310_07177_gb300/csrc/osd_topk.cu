@@ -780,19 +780,20 @@ static osd_status launch_topk(TopParams tp, long long rows, int c, cudaStream_t 
 template <typename In>
 static osd_status launch_topk_dtype(const TopParams& tp, long long rows, cudaStream_t s) {
     const int chunks = static_cast<int>((tp.V + Elem<In>::kVec - 1) / Elem<In>::kVec);
-    // About 16 to 64 chunks a thread: 4096 x 4000 bf16, K = 16 17.5 us with 64 threads a row, 28 with 128; 4096 x 32000,
-    // K = 64 70 us with 128 (64: 89, 256: 82); 1024 x 128256, K = 64 68 us with 128 or 256 (64: 114).  More with a large K
-    // (4096 x 32001, K = 256 109 us, 125 with 128), and where a call leaves SMs idle, while each thread has 4 chunks or more: 512
-    // x 32001, K = 16 12.6 us with 256 threads, 15.7 with 128; and then several CTAs a row: 8 x 128256, K = 16 7.8 us with
-    // four of 512 threads, 10.9 with one.
+    // About 16 to 64 chunks a thread: 4096 x 4000 bf16, K = 16 17.4 us with 64 threads a row, 28 with 128; 4096 x 32000,
+    // K = 64 70 us with 128 (64: 76 to 103, 256: 82); 1024 x 128256, K = 64 68 us with 128 or 256 (64: 114).  Fewer rows at a
+    // time where much is read again, so that L2 still holds them (4096 x 32001 fp32, K = 64 117 us with 256 threads, 121 with
+    // 128, K = 16 100 and 87), and more threads with a large K (4096 x 32001 bf16, K = 256 107 us, 125 with 128) and where a call
+    // leaves SMs idle, while each thread has 4 chunks or more: 512 x 32001, K = 16 12.5 us with 256, 15.7 with 128; and
+    // then several CTAs a row: 8 x 128256, K = 16 7.8 us with four of 512 threads, 10.9 with one.
     const long long slots = (long long)device_sms() * 1024;
-    int t = chunks <= 2048 ? 64 : (chunks <= 8192 ? 128 : (chunks <= 24576 ? 256 : 512)), c = 1;
+    int t = chunks <= 2048 ? 64 : (chunks <= (tp.K < 64 ? 8192 : 4096) ? 128 : (chunks <= 24576 ? 256 : 512)), c = 1;
     while (t < 512 && ((rows * 2 * t <= slots && chunks >= 8 * t) || (t < tp.K && chunks >= 24 * t))) t *= 2;
     while (c < kTopMaxCluster && rows * 2 * t * c <= slots && chunks > 12 * t * c) c *= 2;
     if (t == 512 && rows * c <= device_sms() * (tp.mask ? 2 : 1)) return launch_topk<In, 512, 8, true>(tp, rows, c, s);
-    // sixteen groups a thread halve what is read again, which is much with a large K: 256 x 4 x 128256 fp32, K = 256
-    // 121 us, 128 with eight; but 4096 x 32000 bf16, K = 64 72 us, 70 with eight
-    if (tp.K > 128 && chunks > 8 * t && t >= 256)
+    // sixteen groups a thread halve what is read again, which is much with a large K: 4096 x 32001 fp32, K = 128 130 us,
+    // 142 with eight, 256 x 4 x 128256, K = 256 121 and 128; but 4096 x 32000 bf16, K = 64 72 us, 70 with eight
+    if (tp.K >= 96 && chunks > 8 * t && t >= 256)
         return t == 256 ? launch_topk<In, 256, 16, false>(tp, rows, c, s) : launch_topk<In, 512, 16, false>(tp, rows, c, s);
     switch (t) {
         case 64: return launch_topk<In, 64, 8, false>(tp, rows, c, s);
