@@ -373,8 +373,8 @@ osd_status osd_verify_probs(const void *draft_probs, const void *target_probs, o
  * rest           [G, P] fp32 out, nullable: the natural logarithm of the sum of
  *                exp(x / tau) over the entries not taken; -inf where they are
  *                all -inf or there are none
- * status         nullable device int32, as in osd_distill (rows whose copy did
- *                not arrive in time get ids of -1)
+ * status         nullable device int32, set to 0 (OSD_OK): nothing here waits for a
+ *                copy; kept so that every entry point on rows reports the same way
  * -inf logits are ordinary entries that sort last.  Rows that hold NaN or +inf
  * are outside the domain: their results are unspecified (ids of -1 may occur).
  * Limits: 1 <= V <= OSD_VERIFY_MAX_V, strides >= 0.  No workspace.

@@ -10,6 +10,10 @@
 //
 // Every probability counts as an integer multiple of 2^-62, so the weights
 // max(0, p - q) and all their sums are integers: exact, in any order.
+//
+// Small batches are bound by latency, a chain of launch, tokens, entries, rows, exchange and search: 4 x 4 x
+// 32000 fp32 5.5 us, 32 x 5 x 32000 6.4 us.  Large ones by HBM: 256 x 8 x 128256 fp32 44.4 us, 5.7 TB/s of the rows
+// needed (the kernel itself 40.3 us, 6.5 TB/s), where every row read by every test would be 2.2 GB.
 #include <algorithm>
 #include <climits>
 #include <cstdint>
@@ -42,6 +46,7 @@ struct ProbParams {
     uint8_t* mask;
     int csize;  // CTAs per sequence
     int span;   // vocabulary entries per CTA, whole vectors
+    int ahead;  // the first position's rows start on their way to L2 before the tests
 };
 
 // Sums of weights P - Q in units of 2^-62, where P and Q are p and q rounded to that
@@ -52,14 +57,14 @@ struct ProbParams {
 // pairs, against about 30 with 64-bit shifts.  Half-way cases round to even as a direct
 // rounding to 2^-62 does, since the first two remainders are exact.
 struct FixSum {
-    int hi = 0, mid = 0, lo = 0;
+    uint32_t hi = 0u, mid = 0u, lo = 0u;  // two's complement (rows outside the domain may wrap)
 
     // p, q in pairs; q is taken as min(q, p), so that P - Q is the weight
     template <bool kQ>
     __device__ __forceinline__ void add(float2 p, float2 q) {
         const float2 c1 = f2(2.f), n1 = f2(-2.f), c2 = f2(0x1.8p-21f), n2 = f2(-0x1.8p-21f), c3 = f2(0x1.8p-39f);
         auto part = [](float2 x, const float2& c) { return add2(x, c); };
-        auto bits = [](float x) { return __float_as_int(x); };
+        auto bits = [](float x) { return __float_as_uint(x); };
         const float2 p1 = part(p, c1), rp = sub2(p, add2(p1, n1));
         const float2 p2 = part(rp, c2), sp = sub2(rp, add2(p2, n2));
         const float2 p3 = part(sp, c3);
@@ -72,38 +77,32 @@ struct FixSum {
             mid += (bits(p2.x) - bits(q2.x)) + (bits(p2.y) - bits(q2.y));
             lo += (bits(p3.x) - bits(q3.x)) + (bits(p3.y) - bits(q3.y));
         } else {
-            hi += (bits(p1.x) - 0x40000000) + (bits(p1.y) - 0x40000000);
-            mid += (bits(p2.x) - 0x35400000) + (bits(p2.y) - 0x35400000);
-            lo += (bits(p3.x) - 0x2c400000) + (bits(p3.y) - 0x2c400000);
+            hi += (bits(p1.x) - 0x40000000u) + (bits(p1.y) - 0x40000000u);
+            mid += (bits(p2.x) - 0x35400000u) + (bits(p2.y) - 0x35400000u);
+            lo += (bits(p3.x) - 0x2c400000u) + (bits(p3.y) - 0x2c400000u);
         }
     }
-    __device__ __forceinline__ unsigned long long total() const {
-        return (static_cast<unsigned long long>(static_cast<long long>(hi)) << 40) +
-               (static_cast<unsigned long long>(static_cast<long long>(mid)) << 18) +
-               static_cast<unsigned long long>(static_cast<long long>(lo));
+    __device__ __forceinline__ static unsigned long long wide(uint32_t v) {
+        return static_cast<unsigned long long>(static_cast<long long>(static_cast<int32_t>(v)));
     }
+    __device__ __forceinline__ unsigned long long total() const { return (wide(hi) << 40) + (wide(mid) << 18) + wide(lo); }
     // the warp's total, in every lane: up to 32 entries a lane keep every part within 32 bits, the middle one,
     // at most 2^27 a lane, in two halves
     __device__ __forceinline__ unsigned long long warp_total() const {
-        FixSum s;
-        s.hi = __reduce_add_sync(0xffffffffu, hi);
-        s.lo = __reduce_add_sync(0xffffffffu, lo);
-        s.mid = __reduce_add_sync(0xffffffffu, mid >> 16);
-        const int low = __reduce_add_sync(0xffffffffu, mid & 0xffff);
-        return s.total() - (static_cast<unsigned long long>(static_cast<long long>(s.mid)) << 18) +
-               (static_cast<unsigned long long>(static_cast<long long>(s.mid)) << 34) +
-               (static_cast<unsigned long long>(static_cast<unsigned>(low)) << 18);
+        const uint32_t high = static_cast<uint32_t>(static_cast<int32_t>(mid) >> 16);
+        return (wide(__reduce_add_sync(0xffffffffu, hi)) << 40) + (wide(__reduce_add_sync(0xffffffffu, high)) << 34) +
+               (wide(__reduce_add_sync(0xffffffffu, mid & 0xffffu)) << 18) + wide(__reduce_add_sync(0xffffffffu, lo));
     }
 };
 
-template <typename In> struct Tile {
+struct Tile {
     uint4 p[kProbUnroll], q[kProbUnroll];
 };
 
 // Shared memory of a sequence's draw.
 struct ProbSmem {
     int a, n, y;
-    unsigned long long total, totals[kProbMaxCluster];  // this CTA's, and slot r from CTA r
+    unsigned long long totals[kProbMaxCluster];  // slot r from CTA r
     uint64_t bar;
     unsigned long long W, tau, base;
     int owner, mode, tile;
@@ -131,6 +130,12 @@ __global__ void __launch_bounds__(kProbThreads, 4) verify_probs_kernel(ProbParam
     const int32_t* y = p.tokens + size_t(b) * k;
     const float* u = p.uniforms + size_t(b) * (k + 1);
     int32_t* out = p.out_tokens + size_t(b) * (k + 1);
+    if (kAligned && p.ahead && tid == kT - 1) {
+        const int j = rank * p.span;
+        const uint32_t bytes = static_cast<uint32_t>((min(V, j + p.span) - j) * sizeof(In)) & ~15u;
+        if (bytes) bulk_prefetch_l2(target + j, bytes);
+        if (bytes && draft) bulk_prefetch_l2(draft + j, bytes);
+    }
     // ---- the tests, by every CTA alike: all positions' entries at once, the first failure counts
     if (warp == 0) {
         const int n = p.lens ? p.lens[b] : k;
@@ -200,7 +205,7 @@ __global__ void __launch_bounds__(kProbThreads, 4) verify_probs_kernel(ProbParam
     // ---- the span's weights, a total per sub-tile.  On the 16-byte grid a lane takes vectors
     // of a sub-tile; off it single entries, 32 neighbours a load (shifting vectors into place cost more
     // than the wider loads saved: 600 x 4 x 32001 fp32 44.2 us, against 31.8, bf16 40.1 and 27.4)
-    Tile<In> t;  // the last sub-tile of this warp stays here for the search
+    Tile t;  // the last sub-tile of this warp stays here for the search
     auto vector_at = [&](int s, int i) { return e0 + s * kSub + (i * 32 + lane) * kW; };
     auto load = [&](auto has_q, int s) {
         constexpr bool kQ = decltype(has_q)::value;
@@ -433,6 +438,8 @@ static osd_status launch_probs(ProbParams pp, int B, cudaStream_t s) {
     int c = std::max(1, widest_cluster<verify_probs_kernel<In, kAligned>, kProbThreads>(B, most, kMostSums, true));
     if (c == 1 && most > 1 && row >= 192 * 1024 && B <= device_sms() * 8 / 3) c = 2;
     split_probs(pp.V, c, &pp);
+    // where these rows turn out not to be the ones, so few bytes cost nothing: 32 x 5 x 32000 fp32 6.4 us, 6.9 without
+    pp.ahead = 2 * B * row <= 12000000;
     const size_t smem = size_t((pp.span + kSub - 1) / kSub) * sizeof(unsigned long long);
     if ((long long)B * pp.csize > INT_MAX) return OSD_ERR_UNSUPPORTED;
     return from_cuda(launch_ex(true, verify_probs_kernel<In, kAligned>, dim3(unsigned(B) * unsigned(pp.csize)),
@@ -467,7 +474,7 @@ extern "C" osd_status osd_verify_probs(const void* draft_probs, const void* targ
         !aligned_to(draft_lens, 4) || !aligned_to(uniforms, 4) || !aligned_to(accepted, 4) || !aligned_to(out_tokens, 4))
         return OSD_ERR_INVALID_ARG;
     ProbParams pp = {draft_probs, target_probs, k, V, d_stride_b, d_stride_i, t_stride_b, t_stride_i,
-                     draft_tokens, draft_lens, uniforms, accepted, out_tokens, mismatch_mask, 1, V};
+                     draft_tokens, draft_lens, uniforms, accepted, out_tokens, mismatch_mask, 1, V, 0};
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     return dtype == OSD_BF16 ? launch_probs_dtype<__nv_bfloat16>(pp, B, s) : launch_probs_dtype<float>(pp, B, s);
 }

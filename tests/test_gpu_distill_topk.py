@@ -240,6 +240,40 @@ def test_views_masks_and_given_outputs(osd, dtype):
     assert none.shape == (0,) and nog.shape == (0, V)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_padded_rows_and_gradients_of_any_alignment(osd, dtype):
+    """Rows on the 16-byte grid that end inside a chunk, and gradient buffers off it."""
+    for V, K in ((3, 2), (61, 9), (1001, 40), (33003, 64)):
+        z, top = _inputs(7, V, K, dtype, V)
+        wide = torch.full((7, (V + 15) // 8 * 8), 50.0, dtype=dtype, device="cuda")
+        wide[:, :V] = z.cuda()
+        for off in range(3):
+            buf = torch.full((7 * V + 9,), 7.0, device="cuda")
+            dl = buf[off:off + 7 * V].view(7, V)
+            loss, grad = osd.osd_distill_topk(wide[:, :V], _cuda(top), None, "jsd", dlogits=dl)
+            _compare(loss, grad, z, top, "jsd", 0.5, 1.0)
+            assert (buf[:off] == 7).all() and (buf[off + 7 * V:] == 7).all()
+
+
+def test_largest_rows_and_k(osd):
+    """The longest rows with the most kept tokens fit shared memory; half the ids unused."""
+    for dtype in (torch.float32, torch.bfloat16):
+        z, (v, i, r) = _inputs(2, 393216, 1024, dtype, 23)
+        i[:, ::2] = -1
+        for kind in ("fkl", "rkl"):
+            loss, grad = osd.osd_distill_topk(z.cuda(), _cuda((v, i, r)), None, kind)
+            _compare(loss, grad, z, (v, i, r), kind, 0.5, 1.0)
+
+
+def test_jsd_endpoints(osd):
+    """beta = 0 and beta = 1: loss and gradient 0 (m equals one of the two)."""
+    z, top = _inputs(4, 1000, 20, torch.float32, 24)
+    for beta in (0.0, 1.0):
+        loss, grad = osd.osd_distill_topk(z.cuda(), _cuda(top), None, "jsd", beta)
+        assert loss.abs().max() < 1e-6 and grad.abs().max() < 1e-6
+        _compare(loss, grad, z, top, "jsd", beta, 1.0) if beta == 1.0 else None
+
+
 def test_offsets_past_32_bits(osd):
     V, far = 2000, (1 << 31) + 8 * 13
     z, top = _inputs(2, V, 9, torch.bfloat16, 19)

@@ -137,6 +137,35 @@ def test_views_masks_and_given_outputs(osd, dtype):
     assert (empty.ids.cpu().numpy()[~on] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [3, 61, 1001, 33003])
+def test_padded_rows(osd, dtype, V):
+    """Rows on the 16-byte grid that end inside a chunk: what lies behind them does not count."""
+    x = _normal(9, V, dtype, V)
+    wide = torch.full((9, (V + 15) // 8 * 8), 50.0, dtype=dtype, device="cuda")
+    wide[:, :V] = x.cuda()
+    for K in (1, min(40, V)):
+        got = osd.osd_topk(wide[:, :V], K)
+        v, i, r = compact.topk(x, K)
+        np.testing.assert_array_equal(got.ids.cpu().numpy(), i)
+        _check_rest(got.rest.cpu().numpy().astype(np.float64), r, v, V, 1.0)
+
+
+def test_every_width_of_a_row(osd):
+    """The same rows as part of calls of different sizes, which give a row from 64 threads to several CTAs."""
+    for V, dtype in ((2000, torch.bfloat16), (30000, torch.bfloat16), (130000, torch.float32)):
+        x = _normal(6, V, dtype, V).cuda()
+        many = torch.cat([x] * (100 if V < 100000 else 60))
+        for K in (5, 100, 300):
+            one, few, all_ = osd.osd_topk(x[:1], K), osd.osd_topk(x, K), osd.osd_topk(many, K)
+            v, i, r = compact.topk(x.cpu(), K)
+            for got, n in ((one, 1), (few, 6), (all_, len(many))):
+                np.testing.assert_array_equal(got.ids.cpu().numpy(), np.tile(i, (100, 1))[:n])
+                _check_rest(got.rest.cpu().numpy().astype(np.float64), np.tile(r, 100)[:n], np.tile(v, (100, 1))[:n], V, 1.0)
+            for s, t in zip(all_, osd.osd_topk(many, K)):
+                assert torch.equal(s, t)  # no result depends on the order of atomics
+
+
 def test_offsets_past_32_bits(osd):
     V, far = 2000, (1 << 31) + 8 * 13
     x = _normal(2, V, torch.bfloat16, 6)
@@ -180,8 +209,10 @@ def test_graph_and_streams(osd):
         torch.cuda.synchronize()
         np.testing.assert_array_equal(res.ids.cpu().numpy(), compact.topk(x, 64)[1])
     side.wait_stream(torch.cuda.current_stream())
+    other = b.cuda()
+    torch.cuda.synchronize()
     two = osd.osd_topk(static, 64, stream=side)
-    one = osd.osd_topk(b.cuda(), 64)
+    one = osd.osd_topk(other, 64)
     torch.cuda.synchronize()
     assert torch.equal(two.ids, res.ids) and torch.equal(two.rest, res.rest)
     np.testing.assert_array_equal(one.ids.cpu().numpy(), compact.topk(b, 64)[1])

@@ -91,6 +91,41 @@ def test_strided_views(osd, dtype):
         np.testing.assert_array_equal(a.cpu().numpy(), b)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [3, 61, 1001, 4097, 33003])
+def test_padded_rows(osd, dtype, V):
+    """Rows on the 16-byte grid that end inside a vector, a sub-tile or a span."""
+    B, k, W = 9, 2, (V + 15) // 8 * 8
+    q, p, y, u = _inputs(B, k, V, dtype, V)
+    wide = torch.full((B, k + 1, W), 9.0, dtype=dtype, device="cuda")  # (what lies behind a row is not read as part of it)
+    wide[:, :, :V] = p.cuda()
+    narrow = torch.full((B, k, W), -3.0, dtype=dtype, device="cuda")
+    narrow[:, :, :V] = q.cuda()
+    for d, qq in ((narrow[:, :, :V], q), (None, None)):
+        got = osd.osd_verify_probs(d, wide[:, :, :V], y.cuda(), u.cuda())
+        for a, b in zip(got, compact.verify_probs(qq, p, y.numpy(), u)):
+            np.testing.assert_array_equal(a.cpu().numpy(), b)
+
+
+def test_batches_past_one_wave(osd):
+    """More sequences than the GPU holds at once, with one CTA each and with two."""
+    for B, V, dtype in ((1300, 600, torch.float32), (330, 100000, torch.bfloat16)):
+        q, p, y, u = _inputs(B, 1, V, dtype, B, 0.5)
+        _check(osd, q, p, y, u)
+
+
+def test_two_streams_at_once(osd):
+    cases = [_inputs(40, 3, 32000, torch.float32, 40 + s) for s in range(2)]
+    dev = [[t.cuda() for t in c] for c in cases]
+    streams = [torch.cuda.Stream() for _ in dev]
+    torch.cuda.synchronize()
+    got = [osd.osd_verify_probs(*d, stream=s) for d, s in zip(dev, streams)]
+    torch.cuda.synchronize()
+    for g, (q, p, y, u) in zip(got, cases):
+        for a, b in zip(g, compact.verify_probs(q, p, y.numpy(), u)):
+            np.testing.assert_array_equal(a.cpu().numpy(), b)
+
+
 def test_edges_of_the_draw(osd):
     """Uniforms on the edges of dyadic prefix sums, 0, the largest below 1, and 1; a bonus draw."""
     V = 4096
