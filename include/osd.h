@@ -331,7 +331,7 @@ osd_status osd_verify_tree(const void *draft_logits, const void *target_logits, 
  * it is rounded once, so the token depends on no order of summation.
  *
  * draft_probs    row (b, i) starts at base + b*d_stride_b + i*d_stride_i
- *                elements, V contiguous entries; i < k.  Nullable.
+ *                elements, V contiguous entries; i < k.  Nullable (not read for k = 0).
  * target_probs   the same with t_stride_b, t_stride_i; i <= k
  * draft_tokens   [B, k] int32; entries i >= n are not read
  * draft_lens     [B] int32 in 0..k, nullable (NULL = k everywhere)

@@ -473,7 +473,8 @@ extern "C" osd_status osd_verify_probs(const void* draft_probs, const void* targ
     if (!aligned_to(target_probs, es) || (draft_probs && !aligned_to(draft_probs, es)) || !aligned_to(draft_tokens, 4) ||
         !aligned_to(draft_lens, 4) || !aligned_to(uniforms, 4) || !aligned_to(accepted, 4) || !aligned_to(out_tokens, 4))
         return OSD_ERR_INVALID_ARG;
-    ProbParams pp = {draft_probs, target_probs, k, V, d_stride_b, d_stride_i, t_stride_b, t_stride_i,
+    // (k = 0: no draft row exists)
+    ProbParams pp = {k > 0 ? draft_probs : nullptr, target_probs, k, V, d_stride_b, d_stride_i, t_stride_b, t_stride_i,
                      draft_tokens, draft_lens, uniforms, accepted, out_tokens, mismatch_mask, 1, V, 0};
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     return dtype == OSD_BF16 ? launch_probs_dtype<__nv_bfloat16>(pp, B, s) : launch_probs_dtype<float>(pp, B, s);

@@ -252,3 +252,20 @@ def test_native_equals_ctypes_and_refusals(osd, monkeypatch):
         osd.osd_verify_probs(q, p, y, u, out=osd.VerifyResult(a.accepted[:3], a.out_tokens, a.mismatch_mask, None, None))
     with pytest.raises(TypeError, match="float32 or bfloat16"):
         osd.osd_verify_probs(q.half(), p.half(), y, u)
+
+
+def test_no_draft_row_is_touched_without_drafts(osd):
+    """k = 0: a draft pointer may be given, but no row stands behind it."""
+    import ctypes
+    B, V = 6, 4096
+    _, p, _, u = _inputs(B, 0, V, torch.float32, 77)
+    pd, ud, stub = p.cuda(), u.cuda(), torch.full((4,), float("nan"), device="cuda")
+    acc, out = (torch.full((B,), 9, dtype=torch.int32, device="cuda") for _ in range(2))
+    ptr = lambda t: ctypes.c_void_p(t.data_ptr())
+    assert osd.load_library().osd_verify_probs(
+        ptr(stub), ptr(pd), 0, B, 0, V, 1 << 40, 1 << 40, V, V, None, None, ptr(ud), ptr(acc), ptr(out), None,
+        ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == osd.OSD_OK
+    torch.cuda.synchronize()
+    ref = compact.verify_probs(None, p, np.zeros((B, 0), np.int32), u)
+    np.testing.assert_array_equal(acc.cpu().numpy(), ref[0])
+    np.testing.assert_array_equal(out.cpu().numpy()[:, None], ref[1])
