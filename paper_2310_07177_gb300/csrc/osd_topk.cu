@@ -18,11 +18,13 @@
 // crowded in few groups) go on to the exact K-th largest value, from histograms of all entries,
 // and take the entries equal to it in index order.
 //
-// Not bound by one thing: 4096 x 32000 bf16, K = 64 takes 70 us, 3.8 TB/s, with half of the issue slots in use.  A
+// Not bound by one thing: 4096 x 32000 bf16, K = 64 takes 70 us, 3.8 TB/s, with 56 % of the issue slots in use.  A
 // CTA loads for about half of its life (the sweep); theta, the second reading and the ranking are short dependent steps
-// on little data, which ten CTAs an SM overlap.  fp32, twice the bytes an entry, comes nearer to HBM: 4096 x 32001, K = 16
-// 91 us, 5.8 TB/s.  Measured and left out: the row staged in shared memory by a bulk copy (three CTAs an SM: 92 to 102 us),
-// the whole row read twice (95), a prefetch of the row into L2 (74).
+// on little data, which ten CTAs an SM overlap.  Of 11.7 warp instructions per 32 entries the log-mass takes 5.2 and K = 64
+// instead of 1 2.8 (K = 1 53 us, without the log-mass K = 64 63 us).  fp32, twice the bytes an entry, comes nearer to HBM:
+// 4096 x 32001, K = 16 87 us, 6.0 TB/s.  Measured and left out: the row staged in shared memory by a bulk copy (three CTAs
+// an SM: 92 to 102 us), the whole row read twice (95), a prefetch into L2 of the row (74), or of the one that comes next on
+// the SM (72 to 86).
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -37,7 +39,9 @@ namespace osd {
 
 constexpr int kTopMaxCluster = 8;
 constexpr int kTopBins = 256;        // bins of a histogram over a range of keys
-constexpr int kTopCountMost = 192;   // candidates ranked by counting; more by a histogram of their values
+// Candidates ranked by counting; more by a histogram of their values (4096 x 4000 bf16, K = 40 19.9 us by counting, 20.8 by
+// histogram; K = 150 50 and 33).
+constexpr int kTopCountMost = 96;
 constexpr int kTopCrowd = 48;        // candidates of one bin that are ranked by comparing; with more all are sorted
 // Exponentials (at most 1) of candidates, whose order is that of atomics, are added as whole multiples
 // of 2^-40, so that the sum does not depend on it.
@@ -780,15 +784,22 @@ static osd_status launch_topk(TopParams tp, long long rows, int c, cudaStream_t 
 template <typename In>
 static osd_status launch_topk_dtype(const TopParams& tp, long long rows, cudaStream_t s) {
     const int chunks = static_cast<int>((tp.V + Elem<In>::kVec - 1) / Elem<In>::kVec);
-    // About 16 to 64 chunks a thread: 4096 x 4000 bf16, K = 16 17.4 us with 64 threads a row, 28 with 128; 4096 x 32000,
-    // K = 64 70 us with 128 (64: 76 to 103, 256: 82); 1024 x 128256, K = 64 68 us with 128 or 256 (64: 114).  Fewer rows at a
-    // time where much is read again, so that L2 still holds them (4096 x 32001 fp32, K = 64 117 us with 256 threads, 121 with
-    // 128, K = 16 100 and 87), and more threads with a large K (4096 x 32001 bf16, K = 256 107 us, 125 with 128) and where a call
-    // leaves SMs idle, while each thread has 4 chunks or more: 512 x 32001, K = 16 12.5 us with 256, 15.7 with 128; and
-    // then several CTAs a row: 8 x 128256, K = 16 7.8 us with four of 512 threads, 10.9 with one.
+    // About 16 to 64 chunks a thread: 4096 x 4000 bf16, K = 16 17.4 us with 64 threads a row, 27 with 128; 4096 x 32000,
+    // K = 64 70 us with 128 (64: 83, 256: 80); 1024 x 128256, K = 64 60 us with 256 (128: 65, 64: 91).  Fewer rows at a
+    // time where much is read again, so that L2 still holds them (4096 x 32001 fp32, K = 64 117 us with 256 threads, 120 with
+    // 128, K = 16 100 and 87), and more threads where a call leaves SMs idle, while each thread has 4 chunks or more: 512 x
+    // 32001, K = 16 12.6 us with 256, 13.6 with 128; and then several CTAs a row: 8 x 128256, K = 16 7.8 us with four of 512
+    // threads, 8.7 with one.
     const long long slots = (long long)device_sms() * 1024;
-    int t = chunks <= 2048 ? 64 : (chunks <= (tp.K < 64 ? 8192 : 4096) ? 128 : (chunks <= 24576 ? 256 : 512)), c = 1;
-    while (t < 512 && ((rows * 2 * t <= slots && chunks >= 8 * t) || (t < tp.K && chunks >= 24 * t))) t *= 2;
+    const bool many = tp.K >= 64;
+    int t = chunks <= (many ? 1792 : 2048) ? 64 : (chunks <= (many ? 4096 : 8192) ? 128 : (chunks <= 24576 ? 256 : 512)), c = 1;
+    while (t < 512 && rows * 2 * t <= slots && chunks >= 8 * t) t *= 2;
+    // More threads, so more groups, for a large K.  Three times as many as K for long rows: 4096 x 32000 bf16, K = 350 121 us
+    // with 256 threads, 139 with 128 (K = 256 106 and 102); 4096 x 32000 fp32, K = 700 234 us with 512, 248 with 256 (K = 512
+    // 200 and 186).  Half as many again as K for all that have the chunks, else theta leaves more candidates than there is
+    // room for: 2048 x 12000 bf16, K = 512 59 us, 411 with 64 threads; 4096 x 24000, K = 1000 229, 1157 with 128.  (Rows of
+    // fewer chunks than K go that way all the same: 4096 x 4000, K = 512 258 us.)
+    while (t < 512 && ((tp.K > (t < 256 ? 8 * t / 3 : 640) && chunks >= 20 * t) || (16 * t < 3 * tp.K && chunks > 8 * t))) t *= 2;
     while (c < kTopMaxCluster && rows * 2 * t * c <= slots && chunks > 12 * t * c) c *= 2;
     if (t == 512 && rows * c <= device_sms() * (tp.mask ? 2 : 1)) return launch_topk<In, 512, 8, true>(tp, rows, c, s);
     // sixteen groups a thread halve what is read again, which is much with a large K: 4096 x 32001 fp32, K = 128 130 us,
