@@ -12,17 +12,18 @@
 // ones would cancel), K + 1 classes' worth of arithmetic, and one scaled exponential an entry.
 //
 // One thread-block cluster per row, each CTA with a span of it in shared memory (one bulk
-// copy).  While that flies, every CTA takes the target's distribution from the kept values.  Then the draft's logits at
-// the kept tokens within the span are put aside and -inf in their place; the sums of exponentials of the
+// copy).  While that flies, every CTA reads all kept values: their largest and the sum of their weights against it, and
+// each warp's list of those whose tokens lie within the span.  Then the draft's logits at
+// these are put aside and -inf in their place; the sums of exponentials of the
 // two kinds of entries meet by st.async; each CTA adds up the loss of its kept tokens; and, once the loss's
 // sums have met too (the KL and CE gradients need none of them), a second sweep over the span writes the gradient.
 //
-// Bound by HBM at flush sizes: a row is read and its gradient written once (the registers are capped for
-// ten CTAs of 128 threads an SM, for the KL and CE gradients eight: 8000 x 32000 bf16 FKL, K = 64 230 us, ten: 256; RKL
-// with eight 507 for 469).  16384 x 32000 bf16 RKL, K = 64 469 us, 6.7 TB/s, 99 % of the measured copy bandwidth; 2048 x
-// 128256 FKL, K = 256 271 us (86 %), where a cluster of eight waits for its sums; 16 x 32000 fp32 5.8 us, a chain of copy,
-// two exchanges and stores.  With the draft's logits gathered from global memory by every CTA, and no second
-// exchange, the last took 5.4 us but 4000 x 32000 FKL, K = 512 193 us, where it takes 155.
+// Bound by HBM at flush sizes, where a row is read and its gradient written once: 16384 x 32000 bf16, K = 64, RKL, FKL and
+// JSD 455 to 458 us, 6.9 TB/s, the measured copy bandwidth (64 registers a thread; with 48, 10 CTAs an SM where shared
+// memory allows as many, JSD 489); K = 256 480 (all K by every CTA through every step: 510).  2048 x 128256 FKL, K = 256
+// 246 us (95 %), where a cluster of eight waits for its sums; 16 x 32000 fp32 5.4 us, a chain of copy, two exchanges and
+// stores.  With the draft's logits gathered from global memory by every CTA, and no second
+// exchange, 4000 x 32000 FKL, K = 512 took 193 us, where it takes 138.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -35,14 +36,26 @@
 
 namespace osd {
 
-constexpr int kDtThreads = 128;
-constexpr int kDtWarps = kDtThreads / 32;
-constexpr int kDtMaxCluster = 8;
+constexpr int kDtMaxCluster = 16;  // beyond 8 not portable, but this GPU's own
 constexpr int kDtMaxV = 393216;
 constexpr size_t kDtSpanBytes = 32768;        // of a CTA's span where there are rows enough
+constexpr size_t kDtWideBytes = 60000;        // with longer ones a row takes more than 8 CTAs,
+constexpr size_t kDtLongBytes = 70000;        // or 256 threads a CTA
+constexpr int kDtWideK = 192;                 // (every CTA reads all kept tokens)
 constexpr uint64_t kDtStageWaitNs = 1000000000ull;  // bound on the wait for the bulk copy ...
 constexpr uint64_t kDtPeerWaitNs = 3000000000ull;   // ... and for the peers' sums
 constexpr float kDtRefMax = 4294967296.f;           // a warp's sum past this takes its true maximum
+
+constexpr int kDtBatch = 4;                         // kept tokens a thread reads at a time
+
+// Places of the warps' lists: a warp reads 32 kept tokens of every `threads`.
+__host__ __device__ __forceinline__ constexpr int dt_room(int K, int threads) { return (K + threads - 1) / threads * threads; }
+
+// A kept token in the CTA's span: its position, the target's value and the draft's logit.
+struct DtKept {
+    int at;
+    float v, z;
+};
 
 struct DtParams {
     const void* draft;
@@ -116,6 +129,8 @@ struct DtSums {
     float zmax, dz;    // ... the largest kept logit and its exponent there,
     float w;           // and the probability of an other token per 2^(x c - M)
     float pr, lpr, qr, lqr;
+    float vref, mt, lgL, inv_L;  // the target's largest kept value, what weights are against, their sum
+    int label, empty;
     float coef;     // FKL, CE: of the others' gradient
     int bad;
 };
@@ -123,18 +138,17 @@ struct DtSums {
 // 2^(a - b), 0 for a = -inf
 __device__ __forceinline__ float dt_to_ref(float a, float b) { return a == kNegInf ? 0.f : ex2(a - b); }
 
-template <typename In, int kKind>
-__global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_CE ? 8 : 10) distill_topk_kernel(DtParams p) {
+template <typename In, int kKind, int kT>
+__global__ void __launch_bounds__(kT, 1024 / kT) distill_topk_kernel(DtParams p) {
     using E = Elem<In>;
-    constexpr int kW = E::kVec, kT = kDtThreads;
+    constexpr int kW = E::kVec, kWarps = kT / 32;
     constexpr bool kNoSums = kKind == OSD_FKL || kKind == OSD_CE;  // the gradient needs none of the loss's sums
     extern __shared__ __align__(128) unsigned char dsm[];
-    __shared__ __align__(16) float4 s_recv[2][kDtMaxCluster];  // slot r from CTA r: of the sums, of the loss
     __shared__ __align__(8) uint64_t s_bar, s_peer[2];
-    __shared__ float4 s_part[kDtWarps];
-    __shared__ float3 s_terms[kDtWarps];
-    __shared__ MaxIdx s_best[kDtWarps];
-    __shared__ float s_wl[kDtWarps];
+    __shared__ float4 s_part[kWarps];
+    __shared__ float3 s_terms[kWarps];
+    __shared__ MaxIdx s_best[kWarps];
+    __shared__ float s_wl[kWarps];
     __shared__ DtSums sm;
     __shared__ float4 s_loss;
     __shared__ int s_bad;
@@ -161,10 +175,12 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
     const int c0 = p0 < ph ? 1 : 0;                                  // of which [c0, c1) lie within the row
     const int c1 = max(c0, p0 + n * kW > V + ph ? n - 1 : n);
     In* staged = reinterpret_cast<In*>(dsm);
-    int* s_id = reinterpret_cast<int*>(dsm + size_t(p.span) * sizeof(In));
-    float* s_t = reinterpret_cast<float*>(s_id + K);  // log2 of the target's weight against the largest kept
-    float* s_z = s_t + K;                             // the draft's logits at this CTA's
-    uint32_t* s_seen = reinterpret_cast<uint32_t*>(s_z + K);  // which of this CTA's positions are kept
+    // each warp's list of the kept tokens that it reads and this CTA holds
+    const int room = dt_room(K, kT);
+    DtKept* kept = reinterpret_cast<DtKept*>(dsm + size_t(p.span) * sizeof(In));
+    float4* s_recv = reinterpret_cast<float4*>(kept + room);  // slot r from CTA r: csize of the sums, csize of the loss
+    uint32_t* s_seen = reinterpret_cast<uint32_t*>(s_recv + 2 * csize);  // which of this CTA's positions are kept
+    kept += warp * (room / kWarps);
     if (tid == 0) {
         s_bad = 0;
         mbar_init_only(&s_bar, 1);
@@ -189,45 +205,60 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
     if (c1 < n && c1 >= c0) fringe(n - 1);
     __syncthreads();
 
-    // ---- the target: the kept tokens' values against the largest (with its lowest id)
+    // ---- the target: the kept tokens' weights against the largest (with its lowest id)
     const float ch = p.c_hi, cl = p.c_lo;
     // x c - M of two entries: one rounding after the cancellation, and one of the rest of c, without which the
     // others would weigh up to 5e-7 more or less against the kept tokens
     auto exponents = [ch, cl](float2 x, float M) { return fma2(x, f2(cl), fma2(x, f2(ch), f2(-M))); };
-    auto place = [&](int id) { return id >= 0 ? static_cast<unsigned>(id + ph - p0) : 0xffffffffu; };
-    const unsigned held = static_cast<unsigned>(max(0, p1 - p0));  // this CTA's tokens: place(id) < held
+    const unsigned held = static_cast<unsigned>(max(0, p1 - p0));  // this CTA's tokens: position < held
     MaxIdx best{kNegInf, INT_MAX};
-    for (int i = tid; i < K; i += kT) {
-        int id = p.ids[size_t(row) * K + i];
-        const float v = p.values[size_t(row) * K + i];
-        if (id >= V) {
-            s_bad = 1;
-            id = -1;
-        }
-        if (id >= 0) best = merge_mi(best, MaxIdx{v, id});
-        const unsigned at = place(id);
-        if (at < held && (atomicOr(&s_seen[at >> 5], 1u << (at & 31u)) >> (at & 31u) & 1u)) s_bad = 1;
-        s_id[i] = id;
-        s_t[i] = id >= 0 ? v : kNegInf;
-    }
-    best = warp_reduce(best, [](MaxIdx a, MaxIdx b) { return merge_mi(a, b); });
-    if (lane == 0) s_best[warp] = best;
-    __syncthreads();
+    float L = 0.f;  // sum of exp((v - best) / tau)
+    int n_held = 0;
+    auto weight = [ch, cl](float v, float ref) { return v == kNegInf ? 0.f : ex2(mul_c(v - ref, ch, cl)); };
+    for (int i0 = 0; i0 < K; i0 += kDtBatch * kT) {
+        int id[kDtBatch];
+        float v[kDtBatch];
 #pragma unroll
-    for (int w = 0; w < kDtWarps; ++w) best = merge_mi(best, s_best[w]);
-    const float vref = best.m, rest = (p.rest && kKind != OSD_CE) ? p.rest[row] : kNegInf;
-    const bool empty = fmaxf(vref, rest) == kNegInf;  // no target mass
-    // t_c: log2 of the class's weight against the largest kept value's; mt: their largest
-    const float tr = rest == kNegInf ? kNegInf : (vref == kNegInf ? 0.f : rest_minus(rest, vref, ch, cl));
-    const float mt = vref == kNegInf ? tr : fmaxf(0.f, tr);
-    float L = 0.f;
-    for (int i = tid; i < K; i += kT) {
-        const float v = s_t[i], t = v == kNegInf ? kNegInf : mul_c(v - vref, ch, cl) - mt;
-        s_t[i] = t;
-        L += ex2(t);
+        for (int u = 0; u < kDtBatch; ++u) {  // (all in flight)
+            const int i = i0 + u * kT + tid;
+            id[u] = i < K ? p.ids[size_t(row) * K + i] : -1;
+            v[u] = i < K ? p.values[size_t(row) * K + i] : kNegInf;
+        }
+        const float old = best.m;
+#pragma unroll
+        for (int u = 0; u < kDtBatch; ++u) {
+            if (i0 + u * kT >= K) break;
+            if (id[u] >= V) s_bad = 1;
+            const bool used = id[u] >= 0 && id[u] < V;
+            if (used) best = merge_mi(best, MaxIdx{v[u], id[u]});
+            else v[u] = kNegInf;
+            const unsigned at = used ? static_cast<unsigned>(id[u] + ph - p0) : 0xffffffffu;
+            const bool here = at < held;
+            if (here && (atomicOr(&s_seen[at >> 5], 1u << (at & 31u)) >> (at & 31u) & 1u)) s_bad = 1;
+            const unsigned m = __ballot_sync(0xffffffffu, here);
+            if (here) {
+                const int to = n_held + __popc(m & ((1u << lane) - 1u));
+                kept[to].at = static_cast<int>(at);
+                kept[to].v = v[u];
+            }
+            n_held += __popc(m);
+        }
+        L *= weight(old, best.m);
+#pragma unroll
+        for (int u = 0; u < kDtBatch; ++u) {
+            if (i0 + u * kT >= K) break;
+            L += weight(v[u], best.m);
+        }
     }
-    L = warp_reduce(L, [](float a, float b) { return a + b; });
-    if (lane == 0) s_wl[warp] = L;
+    {
+        const float own = best.m;
+        best = warp_reduce(best, [](MaxIdx a, MaxIdx b) { return merge_mi(a, b); });
+        L = warp_reduce(L * weight(own, best.m), [](float a, float b) { return a + b; });
+        if (lane == 0) {
+            s_best[warp] = best;
+            s_wl[warp] = L;
+        }
+    }
     // ---- the staged span: the kept entries leave it
     bool late = false;
     if (c1 > c0 && !mbar_wait_bounded(&s_bar, 0, kDtStageWaitNs)) {
@@ -235,25 +266,20 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
         mbar_wait_bounded(&s_bar, 0, kDtStageWaitNs);  // give the copy in flight a last chance to land
     }
     float zmax = kNegInf, Zc = 0.f;  // of the warp's kept tokens: the largest logit, the sum of 2^((z - it) c)
-    for (int i = tid; i < K; i += kT) {
-        const unsigned at = place(s_id[i]);
-        if (at < held) {
-            const float z = E::lds(staged + at);
-            E::store(staged + at, kNegInf);
-            s_z[i] = z;
-            zmax = fmaxf(zmax, z);
-        }
+    __syncwarp();
+    for (int i = lane; i < n_held; i += 32) {  // (a lane keeps to its places of the list)
+        const int at = kept[i].at;
+        const float z = E::lds(staged + at);
+        E::store(staged + at, kNegInf);
+        kept[i].z = z;
+        zmax = fmaxf(zmax, z);
     }
     zmax = warp_reduce(zmax, [](float a, float b) { return fmaxf(a, b); });
     if (zmax != kNegInf) {
-        for (int i = tid; i < K; i += kT)
-            if (place(s_id[i]) < held) Zc += ex2(mul_c(s_z[i] - zmax, ch, cl));
+        for (int i = lane; i < n_held; i += 32) Zc += ex2(mul_c(kept[i].z - zmax, ch, cl));
         Zc = warp_reduce(Zc, [](float a, float b) { return a + b; });
     }
     const bool failed = __syncthreads_or(late);
-    L = ex2(tr - mt);
-#pragma unroll
-    for (int w = 0; w < kDtWarps; ++w) L += s_wl[w];
     // ---- the others' exponentials against the warp's reference, the largest entry of its first chunks: sums past
     // 2^32, and warps whose first chunks hold nothing, take the true maximum first
     const float2 mine = [&]() {
@@ -293,7 +319,7 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
     if (csize > 1) cluster_wait();
     auto push = [&](int which, float4 v, int to) {  // warp 0: to the first CTAs of the cluster
         if (lane < to)
-            st_async_v4(map_rank(&s_recv[which][rank], static_cast<uint32_t>(lane)), v,
+            st_async_v4(map_rank(s_recv + which * csize + rank, static_cast<uint32_t>(lane)), v,
                         map_rank(&s_peer[which], static_cast<uint32_t>(lane)));
         if (lane == 0 && rank < to) mbar_arrive_expect_tx(&s_peer[which], static_cast<uint32_t>(csize) * 16u);
     };
@@ -301,7 +327,7 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
         return __all_sync(0xffffffffu, mbar_wait_cluster_bounded(&s_peer[which], 0, kDtPeerWaitNs)) != 0;
     };
     if (warp == 0) {
-        float4 v = lane < kDtWarps ? s_part[lane] : make_float4(kNegInf, 0.f, kNegInf, 0.f);
+        float4 v = lane < kWarps ? s_part[lane] : make_float4(kNegInf, 0.f, kNegInf, 0.f);
         auto merge = [&](float4& w) {
             const float m = warp_reduce(w.x, [](float a, float b) { return fmaxf(a, b); });
             const float z = warp_reduce(w.z, [](float a, float b) { return fmaxf(a, b); });
@@ -316,14 +342,36 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
         float flags = fminf(v.y, 0.f);
         if (csize > 1) {
             push(0, v, csize);
+        }
+        // the target's side, in the meantime
+        best = s_best[0];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) best = merge_mi(best, s_best[w]);
+        const float vref = best.m, rest = (p.rest && kKind != OSD_CE) ? p.rest[row] : kNegInf;
+        // log2 of the weights against the largest kept value's: tr of the rest, mt of the largest
+        const float tr = rest == kNegInf ? kNegInf : (vref == kNegInf ? 0.f : rest_minus(rest, vref, ch, cl));
+        const float mt = vref == kNegInf ? tr : fmaxf(0.f, tr);
+        L = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) L = fmaf(s_wl[w], weight(s_best[w].m, vref), L);
+        L = fmaf(L, ex2(-mt), ex2(tr - mt));
+        DtSums r;
+        r.vref = vref;
+        r.mt = mt;
+        r.lgL = log2f(L);
+        r.inv_L = 1.f / L;
+        r.label = best.i;
+        r.empty = fmaxf(vref, rest) == kNegInf;
+        r.lpr = kKind == OSD_CE ? kNegInf : (tr - mt) - r.lgL;
+        r.pr = kKind == OSD_CE ? 0.f : ex2(tr - mt) * r.inv_L;
+        if (csize > 1) {
             gone = !arrived(0);
-            v = lane < csize && !gone ? s_recv[0][lane] : make_float4(kNegInf, 0.f, kNegInf, 0.f);
+            v = lane < csize && !gone ? s_recv[lane] : make_float4(kNegInf, 0.f, kNegInf, 0.f);
             flags = warp_reduce(fminf(v.y, 0.f), [](float a, float b) { return fminf(a, b); });
             merge(v);
         }
         zmax = v.z;
         Zc = v.w;
-        DtSums r;
         r.M = v.x;
         r.S = v.y;
         const bool others = r.M != kNegInf;
@@ -337,8 +385,6 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
         r.w = others ? ex2(-mx) * r.inv_Z : 0.f;
         r.qr = r.S * r.w;
         r.lqr = others ? (log2f(r.S) - mx) - r.lgZ : kNegInf;
-        r.lpr = kKind == OSD_CE ? kNegInf : (tr - mt) - log2f(L);
-        r.pr = kKind == OSD_CE ? 0.f : ex2(tr - mt) / L;
         r.coef = others ? r.w - (r.pr > 0.f ? r.pr / r.S : 0.f) : 0.f;
         r.zmax = zmax;
         r.bad = gone || flags < -1.f ? 2 : (flags < 0.f ? 1 : 0);
@@ -346,7 +392,7 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
     }
     __syncthreads();
     const DtSums r = sm;
-    const bool dead_row = r.bad || empty;
+    const bool dead_row = r.bad || r.empty;
     if (r.bad == 2) {  // a copy or a peer's sum did not arrive in time
         if (tid == 0) {
             if (rank == 0) p.loss[row] = __int_as_float(0x7fc00000);
@@ -355,24 +401,23 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
         return;
     }
     // ---- the classes, by every CTA alike
-    const float lgL = log2f(L), inv_L = 1.f / L;
     auto target = [&](int i, float& pc, float& lp) {
         if constexpr (kKind == OSD_CE) {
-            pc = s_id[i] == best.i ? 1.f : 0.f;
+            pc = kept[i].at + p0 - ph == r.label ? 1.f : 0.f;
             lp = pc > 0.f ? 0.f : kNegInf;
         } else {
-            pc = ex2(s_t[i]) * inv_L;
-            lp = s_t[i] - lgL;
+            const float v = kept[i].v, t = v == kNegInf ? kNegInf : mul_c(v - r.vref, ch, cl) - r.mt;
+            pc = ex2(t) * r.inv_L;
+            lp = t - r.lgL;
         }
     };
     auto draft = [&](int i, float& qc, float& lq) {
-        const float z = s_z[i], e = z == kNegInf ? kNegInf : mul_c(z - r.zmax, ch, cl) + r.dz;
+        const float z = kept[i].z, e = z == kNegInf ? kNegInf : mul_c(z - r.zmax, ch, cl) + r.dz;
         qc = ex2(e) * r.inv_Z;
         lq = e - r.lgZ;
     };
     float3 s = rank == 0 && tid == 0 ? class_terms<kKind>(r.pr, r.lpr, r.qr, r.lqr, p.beta) : make_float3(0.f, 0.f, 0.f);
-    for (int i = tid; i < K; i += kT) {
-        if (place(s_id[i]) >= held) continue;
+    for (int i = lane; i < n_held; i += 32) {
         float pc, lp, qc, lq;
         target(i, pc, lp);
         draft(i, qc, lq);
@@ -386,7 +431,7 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
     if (warp == 0) {
         s = s_terms[0];
 #pragma unroll
-        for (int w = 1; w < kDtWarps; ++w) s = add3(s, s_terms[w]);
+        for (int w = 1; w < kWarps; ++w) s = add3(s, s_terms[w]);
         if (csize > 1) push(1, make_float4(s.x, s.y, s.z, 0.f), kNoSums ? 1 : csize);
     }
     // the loss's sums over the cluster, in every thread; false if a peer's did not arrive in time
@@ -396,7 +441,7 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
             if (csize > 1) {
                 got = arrived(1);
                 s = make_float3(0.f, 0.f, 0.f);
-                for (int q = 0; q < csize && got; ++q) s = add3(s, make_float3(s_recv[1][q].x, s_recv[1][q].y, s_recv[1][q].z));
+                for (int q = 0; q < csize && got; ++q) s = add3(s, make_float3(s_recv[csize + q].x, s_recv[csize + q].y, s_recv[csize + q].z));
             }
             if (lane == 0) s_loss = make_float4(s.x, s.y, s.z, got ? 0.f : 1.f);
         }
@@ -407,7 +452,7 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
     float loss = 0.f;
     auto write_loss = [&](bool got) {
         if (tid == 0) {
-            if (rank == 0) p.loss[row] = r.bad || !got ? __int_as_float(0x7fc00000) : (empty ? 0.f : loss);
+            if (rank == 0) p.loss[row] = r.bad || !got ? __int_as_float(0x7fc00000) : (r.empty ? 0.f : loss);
             if (p.status && (!got || (rank == 0 && r.bad)))
                 atomicExch(p.status, static_cast<int32_t>(got ? OSD_ERR_INVALID_ARG : OSD_ERR_TIMEOUT));
         }
@@ -454,8 +499,7 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
         for (int i = tid; i < n * kW; i += kT) entry(i);
     }
     __syncthreads();
-    for (int i = tid; i < K; i += kT) {
-        if (place(s_id[i]) >= held) continue;
+    for (int i = lane; i < n_held; i += 32) {
         float pc, lp, qc, lq, g = 0.f;
         target(i, pc, lp);
         draft(i, qc, lq);
@@ -463,12 +507,34 @@ __global__ void __launch_bounds__(kDtThreads, kKind == OSD_FKL || kKind == OSD_C
             if constexpr (kNoSums) g = qc - pc;
             else if (qc > 0.f) g = qc * class_factor<kKind>(pc, lp, qc, lq, s, loss, p.beta);
         }
-        out[s_id[i]] = g * p.inv_tau;
+        out[p0 + kept[i].at - ph] = g * p.inv_tau;
     }
     if (kNoSums && rank == 0) {
         const bool got = loss_sums();
         loss = class_loss<kKind>(s, p.beta);
         write_loss(got);
+    }
+}
+
+template <typename In, int kT>
+static osd_status launch_distill_topk_of(osd_loss kind, const DtParams& dp, long long rows, cudaStream_t s) {
+    const size_t smem = size_t(dp.span) * sizeof(In) + size_t(dt_room(dp.K, kT)) * sizeof(DtKept) +
+                        size_t(dp.csize) * 2 * sizeof(float4) + size_t((dp.span + 31) / 32) * 4;
+    auto go = [&](auto kind_tag) -> osd_status {
+        constexpr int kKind = decltype(kind_tag)::value;
+        if (dp.csize > 8 && cudaFuncSetAttribute(distill_topk_kernel<In, kKind, kT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
+                                cudaSuccess)
+            return OSD_ERR_CUDA;
+        if (ctas_per_sm<distill_topk_kernel<In, kKind, kT>, kT>(smem) < 1) return OSD_ERR_CUDA;  // (opts in for the size)
+        return from_cuda(launch_ex(true, distill_topk_kernel<In, kKind, kT>, dim3(static_cast<unsigned>(rows * dp.csize)), dim3(kT),
+                                   smem, s, dp.csize, dp));
+    };
+    switch (kind) {
+        case OSD_FKL: return go(std::integral_constant<int, OSD_FKL>());
+        case OSD_RKL: return go(std::integral_constant<int, OSD_RKL>());
+        case OSD_JSD: return go(std::integral_constant<int, OSD_JSD>());
+        case OSD_TVD: return go(std::integral_constant<int, OSD_TVD>());
+        default: return go(std::integral_constant<int, OSD_CE>());
     }
 }
 
@@ -478,27 +544,19 @@ static osd_status launch_distill_topk(osd_loss kind, DtParams dp, long long rows
     const int positions = dp.V + Elem<In>::kVec - 1;  // a row starts up to kVec - 1 positions into the grid
     // Spans of 32 KB: 16384 x 32000 bf16 RKL 469 us (16 KB: 537, 8 KB: 900; 64 KB: 464, but 128.2 us against 122.4 for
     // 8192 x 32001 JSD at 40 % active and 319 against 298 for 2048 x 128256 FKL).  A call that leaves SMs idle takes
-    // shorter ones, from 8 KB on (8 x 32000 bf16 RKL 5.8 us, 7.3 with 32 KB).
-    int c = static_cast<int>((size_t(positions) * es + kDtSpanBytes - 1) / kDtSpanBytes);
-    while (c < kDtMaxCluster && rows * 2 * c <= 2 * device_sms() && size_t(positions) * es / (2 * c) >= 8000) c *= 2;
-    c = std::min(c, kDtMaxCluster);
+    // shorter ones, from 8 KB on (8 x 32000 bf16 RKL 5.5 us, 7.3 with 32 KB).  Rows too long for eight of 60 KB take
+    // sixteen CTAs: 1024 x 160000 fp32 FKL, K = 64 213 us, 245 with eight; but K = 300 269 and 248.
+    const size_t bytes = size_t(positions) * es;
+    int c = static_cast<int>((bytes + kDtSpanBytes - 1) / kDtSpanBytes);
+    while (c < 8 && rows * 2 * c <= 2 * device_sms() && bytes / (2 * c) >= 8000) c *= 2;
+    c = std::min(c, bytes > 8 * kDtWideBytes && dp.K <= kDtWideK ? kDtMaxCluster : 8);
     dp.span = ((positions + c - 1) / c + 63) / 64 * 64;
     dp.csize = (positions + dp.span - 1) / dp.span;
     if (rows * dp.csize > INT_MAX) return OSD_ERR_UNSUPPORTED;
-    const size_t smem = size_t(dp.span) * es + size_t(dp.K) * 12 + size_t((dp.span + 31) / 32) * 4;
-    auto go = [&](auto kind_tag) -> osd_status {
-        constexpr int kKind = decltype(kind_tag)::value;
-        if (ctas_per_sm<distill_topk_kernel<In, kKind>, kDtThreads>(smem) < 1) return OSD_ERR_CUDA;  // (opts in for the size)
-        return from_cuda(launch_ex(true, distill_topk_kernel<In, kKind>, dim3(static_cast<unsigned>(rows * dp.csize)),
-                                   dim3(kDtThreads), smem, s, dp.csize, dp));
-    };
-    switch (kind) {
-        case OSD_FKL: return go(std::integral_constant<int, OSD_FKL>());
-        case OSD_RKL: return go(std::integral_constant<int, OSD_RKL>());
-        case OSD_JSD: return go(std::integral_constant<int, OSD_JSD>());
-        case OSD_TVD: return go(std::integral_constant<int, OSD_TVD>());
-        default: return go(std::integral_constant<int, OSD_CE>());
-    }
+    // 256 threads where only two spans fit an SM: 1024 x 160000 fp32 FKL, K = 300 248 us, 266 with 128; but 1024 x 250000
+    // bf16 (62 KB) 296 and 268
+    return size_t(dp.span) * es > kDtLongBytes ? launch_distill_topk_of<In, 256>(kind, dp, rows, s)
+                                               : launch_distill_topk_of<In, 128>(kind, dp, rows, s);
 }
 
 }  // namespace osd

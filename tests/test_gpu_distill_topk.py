@@ -97,7 +97,7 @@ def test_small(osd, kind, dtype):
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("N,V,K", [(40, 32000, 64), (6, 32001, 100), (2, 128256, 256), (1, 160007, 1024), (400, 2999, 8),
-                                   (3, 393216, 17)])
+                                   (3, 393216, 17), (4, 130001, 190), (4, 130001, 200), (2, 100000, 513)])
 def test_large(osd, N, V, K, dtype, kind):
     z, top = _inputs(N, V, K, dtype, N + V, 2.0)
     used = _check(osd, z, top, kind, 0.5, 2.0)
