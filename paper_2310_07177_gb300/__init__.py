@@ -12,6 +12,11 @@ no CPU path.  If the library has not been built, calls raise immediately.
                uniforms [B,k+1], temperature)           # Appendix A.1, Algorithm 1
     osd_distill(draft_logits [..,V], target_logits [..,V], mask, loss_kind, beta)
                                                        # Eq. 2-3, Section 4.1
+    osd_verify_probs(draft_probs [B,k,V] or None, target_probs [B,k+1,V], draft_tokens [B,k],
+                     uniforms [B,k+1], draft_lens=[B] or None)   # given probabilities
+    osd_topk(logits [..,V], K, mask, temperature)       # compact rows of buffer R
+    osd_distill_topk(draft_logits [..,V], (values [..,K], ids [..,K], rest [..]), mask,
+                     loss_kind, beta)                  # osd_distill against such rows
 """
 from __future__ import annotations
 
