@@ -801,7 +801,16 @@ static osd_status launch_topk_dtype(const TopParams& tp, long long rows, cudaStr
     // fewer chunks than K go that way all the same: 4096 x 4000, K = 512 258 us.)
     while (t < 512 && ((tp.K > (t < 256 ? 8 * t / 3 : 640) && chunks >= 20 * t) || (16 * t < 3 * tp.K && chunks > 8 * t))) t *= 2;
     while (c < kTopMaxCluster && rows * 2 * t * c <= slots && chunks > 12 * t * c) c *= 2;
-    if (t == 512 && rows * c <= device_sms() * (tp.mask ? 2 : 1)) return launch_topk<In, 512, 8, true>(tp, rows, c, s);
+    // (several CTAs a row: as many as one wave holds, half of the rows of a mask: 18 x 102708 fp32, K = 64 9.2 us with clusters
+    // of six, 14.4 in two waves of eight; 76 x 128256 bf16, K = 14 12.9 with three, 16.8 with four)
+    const bool few = t == 512 && rows * c <= device_sms() * (tp.mask ? 2 : 1);
+    if (c > 1) {
+        constexpr size_t kSmem = 32768;  // about what such a CTA takes
+        const long long active = tp.mask ? (rows + 1) / 2 : rows, clusters = active + active / 16;  // (with some to spare)
+        c = few ? widest_cluster<topk_kernel<In, true, 512, 8, true>, 512>(clusters, c, kSmem, true)
+                : widest_cluster<topk_kernel<In, true, 512, 8, false>, 512>(clusters, c, kSmem, true);
+    }
+    if (few) return launch_topk<In, 512, 8, true>(tp, rows, c, s);
     // sixteen groups a thread halve what is read again, which is much with a large K: 4096 x 32001 fp32, K = 128 130 us,
     // 142 with eight, 256 x 4 x 128256, K = 256 121 and 128; but 4096 x 32000 bf16, K = 64 72 us, 70 with eight
     if (tp.K >= 96 && chunks > 8 * t && t >= 256)
