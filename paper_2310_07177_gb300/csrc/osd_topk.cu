@@ -362,7 +362,10 @@ __global__ void __launch_bounds__(kT, kFew ? 1 : (kT == 128 ? 1280 : 1024) / kT)
         const int at = atomicAdd(&sh.n, 1);
         if (at < p.room) cand[at] = cand_of(v, j);
     };
-    {
+    const bool all = T == kKeyNegInf && V > p.room;  // every entry would be a candidate: no room for them
+    if (all) {
+        over = true;
+    } else {
         const bool far = kRest && !(M - Mt <= 20.f);
         const float scale = far ? 0.f : ex2(M - Mt);
         int hits = 0;
@@ -503,24 +506,30 @@ __global__ void __launch_bounds__(kT, kFew ? 1 : (kT == 128 ? 1280 : 1024) / kT)
         slow = n > p.room;
     }
     float log_ref = mul_c(Mt, kLn2, kLn2Lo);  // the logarithm of what the sum is against
+    // every entry of this CTA once, in no order
+    auto each = [&](auto f) {
+        for (int v = v0; v < c1; v += kT) {
+            float y[kW];
+            E::unpack(ldg_nc(body + size_t(v) * kW), y);
+#pragma unroll
+            for (int e = 0; e < kW; ++e) f(y[e], v * kW + e - ph);
+        }
+        if (tid < singles) f(E::load(x + single(tid)), single(tid));
+    };
     // the sum of the entries' exponentials below `bound` over the cluster, against the largest of them, m
     auto below = [&](float bound, float& m) {
         float mx = kNegInf;
-#pragma unroll 8
-        for (int j = first + tid; j < end; j += kT) {
-            const float v = E::load(x + j);
+        each([&](float v, int) {
             if (v < bound) mx = fmaxf(mx, v);
-        }
+        });
         mx = block_reduce<kT>(mx, [](float a, float b) { return fmaxf(a, b); }, sh.warp_f);
         const TopPart* q = exchange(TopPart{0, 0, 0.f, mx});
         for (int r = 0; r < csize; ++r) mx = fmaxf(mx, q[r].top);
         float sum = 0.f;
         if (mx != kNegInf) {
-#pragma unroll 8
-            for (int j = first + tid; j < end; j += kT) {
-                const float v = E::load(x + j);
+            each([&](float v, int) {
                 if (v < bound) sum += ex2((v - mx) * c);
-            }
+            });
         }
         sum = block_reduce<kT>(sum, [](float a, float b) { return a + b; }, sh.warp_f);
         q = exchange(TopPart{0, 0, sum, 0.f});
@@ -543,11 +552,10 @@ __global__ void __launch_bounds__(kT, kFew ? 1 : (kT == 128 ? 1280 : 1024) / kT)
             } else {
                 __syncthreads();
             }
-#pragma unroll 4
-            for (int j = first + tid; j < end; j += kT) {
-                const uint32_t k = key_of(E::load(x + j));
+            each([&](float v, int) {
+                const uint32_t k = key_of(v);
                 if (k >= lo && k <= hi) atomicAdd(&sh.hist[(k - lo) >> shift], 1);
-            }
+            });
             __syncthreads();
             if (rank > 0)
                 for (int i = tid; i < kTopBins; i += kT)
@@ -568,17 +576,15 @@ __global__ void __launch_bounds__(kT, kFew ? 1 : (kT == 128 ? 1280 : 1024) / kT)
             hi = min(hi, kth + ((1u << shift) - 1u));
         }
         T = kth;
-        // the entries above it, then those equal to it, in index order: warps own runs of entries
+        // the entries above it, then those equal to it, where they are too many in index order: warps own runs of entries
         if (tid == 0) sh.n = 0;
         __syncthreads();
         int equal = 0;
-        for (int j0 = first + warp * 32; j0 < end; j0 += kT) {
-            const bool in = j0 + lane < end;
-            const float v = in ? E::load(x + j0 + lane) : 0.f;
+        each([&](float v, int j) {
             const uint32_t k = key_of(v);
-            if (in && k > kth) append(v, j0 + lane);
-            equal += in && k == kth ? 1 : 0;
-        }
+            if (k > kth) append(v, j);
+            equal += k == kth ? 1 : 0;
+        });
         __syncthreads();
         const int above = min(sh.n, p.room);
         equal = block_sum(equal);
@@ -590,9 +596,14 @@ __global__ void __launch_bounds__(kT, kFew ? 1 : (kT == 128 ? 1280 : 1024) / kT)
             all_equal += parts[r].m;
         }
         const int quota = max(0, min(equal, K - all_above - lower));  // how many of the equal ones here are taken
-        {
-            const int per = ((end - first + kWarps - 1) / kWarps + 31) / 32 * 32;
-            const int lo = min(end, first + warp * per), hi = min(end, lo + per);
+        if (quota == equal) {  // all of them: no need for their order
+            each([&](float v, int j) {
+                if (key_of(v) == kth) append(value_of(kth), j);
+            });
+            __syncthreads();
+        } else {
+            const int run = ((end - first + kWarps - 1) / kWarps + 31) / 32 * 32;
+            const int lo = min(end, first + warp * run), hi = min(end, lo + run);
             auto is = [&](int j) { return j < hi && key_of(E::load(x + j)) == kth; };
             int mine = 0;
             for (int j = lo; j < hi; j += 32) mine += __popc(__ballot_sync(0xffffffffu, is(j + lane)));
@@ -798,7 +809,7 @@ static osd_status launch_topk_dtype(const TopParams& tp, long long rows, cudaStr
     // with 256 threads, 139 with 128 (K = 256 106 and 102); 4096 x 32000 fp32, K = 700 234 us with 512, 248 with 256 (K = 512
     // 200 and 186).  Half as many again as K for all that have the chunks, else theta leaves more candidates than there is
     // room for: 2048 x 12000 bf16, K = 512 59 us, 411 with 64 threads; 4096 x 24000, K = 1000 229, 1157 with 128.  (Rows of
-    // fewer chunks than K go that way all the same: 4096 x 4000, K = 512 258 us.)
+    // fewer chunks than K go that way all the same: 4096 x 4000, K = 512 205 us.)
     while (t < 512 && ((tp.K > (t < 256 ? 8 * t / 3 : 640) && chunks >= 20 * t) || (16 * t < 3 * tp.K && chunks > 8 * t))) t *= 2;
     while (c < kTopMaxCluster && rows * 2 * t * c <= slots && chunks > 12 * t * c) c *= 2;
     // (several CTAs a row: as many as one wave holds, half of the rows of a mask: 18 x 102708 fp32, K = 64 9.2 us with clusters
