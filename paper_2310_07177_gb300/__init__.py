@@ -24,6 +24,7 @@ import contextlib
 import ctypes
 import importlib.machinery
 import importlib.util
+import operator
 import os
 import warnings
 from typing import NamedTuple, Optional
@@ -452,14 +453,16 @@ def osd_topk(logits: torch.Tensor, K: int, mask: Optional[torch.Tensor] = None, 
     lib = load_library()
     dev = _need_cuda(logits, mask, status, *(out or ()))
     G, P, V, sg, sp = _rows_view(logits)
-    K = int(K)
+    K = operator.index(K)
     lead = tuple(logits.shape[:-1])
+    if status is not None and status.dtype != torch.int32:
+        raise ValueError("status must be int32")
     if mask is not None and (mask.dtype != torch.uint8 or tuple(mask.shape) != lead or not mask.is_contiguous()):
         raise ValueError("mask must be contiguous uint8 with the logits' leading shape")
     dt = _dtype_code(logits)
     if out is None:
-        if K < 1:
-            raise OsdError(OSD_ERR_INVALID_ARG, "osd_topk")
+        if not 1 <= K <= min(V, TOPK_MAX_K):  # (before the outputs are allocated)
+            raise OsdError(OSD_ERR_UNSUPPORTED if TOPK_MAX_K < K <= V else OSD_ERR_INVALID_ARG, "osd_topk")
         out = TopkResult(torch.empty(*lead, K, dtype=torch.float32, device=dev),
                          torch.empty(*lead, K, dtype=torch.int32, device=dev),
                          torch.empty(lead, dtype=torch.float32, device=dev) if rest else None)

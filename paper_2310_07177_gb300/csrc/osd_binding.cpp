@@ -337,7 +337,7 @@ PyObject* topk(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int dt = dtype_code(*x);
         const long K = PyLong_AsLong(a[1]);
         if (K == -1 && PyErr_Occurred()) PyErr_Clear();
-        c.need(dt >= 0 && K >= 1 && K <= INT_MAX);
+        c.need(dt >= 0 && K >= 1 && K <= OSD_TOPK_MAX_K && K <= r.V);
         const at::Tensor *mask = c.optional(a[2]), *status = c.optional(a[6]);
         const double temperature = c.number(a[3]);
         const bool rest = a[4] == Py_True;

@@ -57,7 +57,8 @@ def test_sizes(osd, V, dtype):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("N,V,K", [(300, 32000, 64), (20, 32001, 33), (3, 128256, 256), (1, 160007, 1024), (2, 70000, 1),
-                                   (1, 600001, 512), (700, 3001, 16)])
+                                   (1, 600001, 512), (700, 3001, 16), (18, 102708, 64), (76, 70001, 12), (400, 12000, 512),
+                                   (200, 24000, 1000), (300, 16001, 97), (20, 4001, 800)])
 def test_large(osd, N, V, K, dtype):
     _check(osd, _normal(N, V, dtype, N + V), K, 2.0 if K == 33 else 1.0)
 
@@ -235,6 +236,15 @@ def test_native_equals_ctypes_and_refusals(osd, monkeypatch):
     for K in (0, -1, 901, 1025):
         with pytest.raises(osd.OsdError):
             osd.osd_topk(x, K)
+    free = torch.cuda.memory_allocated()
+    for K, status in ((2 ** 31 - 1, osd.OSD_ERR_INVALID_ARG), (1 << 40, osd.OSD_ERR_INVALID_ARG)):
+        with pytest.raises(osd.OsdError) as refused:  # before outputs of that size are allocated
+            osd.osd_topk(x, K)
+        assert refused.value.status == status and torch.cuda.memory_allocated() == free
+    with pytest.raises(TypeError):
+        osd.osd_topk(x, 5.5)
+    with pytest.raises(ValueError, match="status"):
+        osd.osd_topk(x, 5, status=torch.zeros(1, dtype=torch.int8, device="cuda"))
     with pytest.raises(osd.OsdError):
         osd.osd_topk(x, 5, temperature=0.0)
     with pytest.raises(ValueError, match="mask"):
